@@ -264,6 +264,77 @@ int specroll_gather_hidden(int32_t B, int32_t N, int32_t d, const void *hidden,
                            const int32_t *term_node, void *h_next, void *cuda_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Page tables and slot maps of a paged cache, made on the GPU from the sequences' lengths (the paper has no counterpart; the
+ * layout is the one above).  In one launch, nothing is read back.  For sequence b with kv_len[b] tokens in the cache (a negative
+ * length counts as 0) and the pages page_table[page_indptr[b] .. page_indptr[b + 1]):
+ *   add[b] >= 0  it is about to take add[b] tokens: it keeps its pages and gets as many more as kv_len[b] + add[b] tokens need
+ *   add[b] <  0  it has finished: its pages go back, it owns none
+ * New pages come from the front of free_list[0 .. *n_free) in the order of the sequences, and the pages given back go behind
+ * what is left of it, in the order of the sequences and of their tables.  (They are handed out from the next call on.)
+ * Outputs: page_table_out[table_cap] and page_indptr_out[B + 1], the new tables; tok_indptr[B + 1] and slot_map[slot_cap], where
+ * slot_map[tok_indptr[b] + i] = page * 128 + place is the slot of position kv_len[b] + i, i < add[b], as
+ * specroll_kv4_store takes it; free_list_out[free_cap] and *n_free_out.  Entries behind the last one are -1 in all three arrays,
+ * and so are pages that the free list did not have and the slots on them.  When it runs out, or an array is too short (what does
+ * not fit is not written), *status (device word, nullable; never cleared here) becomes SPECROLL_ELIMIT.
+ * n_table: entries of page_table (it is not read beyond them).  Outputs must not overlap inputs.
+ * All pointers device; slot_map i64 and 16-byte aligned, the others i32; B <= 4096 (else SPECROLL_ELIMIT), free_cap <= 2^24.
+ * With B = 0 the tables are empty and the free list stays as it is. */
+int specroll_page_plan(int32_t B, const int32_t *kv_len, const int32_t *add, const int32_t *page_table, int32_t n_table,
+                       const int32_t *page_indptr, const int32_t *free_list, int32_t free_cap, const int32_t *n_free,
+                       int32_t table_cap, int64_t slot_cap, int32_t *page_table_out, int32_t *page_indptr_out,
+                       int32_t *tok_indptr, int64_t *slot_map, int32_t *free_list_out, int32_t *n_free_out,
+                       int32_t *status, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A paged cache held in 4 bits (the paper has no counterpart): 17 bytes for 32 elements where bf16 takes 64.
+ *
+ * The 32 elements 32 i .. 32 i + 31 of a token's head share a scale s, a byte 8 e + m (m < 8, e < 32) that stands for
+ * (8 + m) 2^(e - 23); an element is q s with a whole number q, -8 <= q <= 7.  Every such value is exact in bf16.  Writing: s is
+ * max|x| / 7 rounded to four significant bits (halves up; between 2^-20 and 15 * 2^8), q is x / s rounded to the nearest whole
+ * number (halves away from zero), into [-8, 7].  NaN is stored as 0, an infinity as the largest value of its sign.
+ * A layer's pool is u8 [n_pages, Hkv, 2 (K, then V), tile] with tile = specroll_kv4_tile_bytes(D) = 128 (D/2 + D/32): the
+ * codes q + 8 of the page's 128 tokens [128][D/2], then their scales [128][D/32].  In the 32-bit word (little endian) of eight
+ * neighbouring elements, element 2 j has bits 4 j .. 4 j + 3 and element 2 j + 1 bits 16 + 4 j .. 19 + 4 j.  Any bytes decode to
+ * finite values: rows of a page beyond a sequence's length may hold anything.
+ * D == 64 or 128; the pool's base is 16-byte aligned; n_pages <= 2^24. */
+size_t specroll_kv4_tile_bytes(int32_t D);
+
+/* K, V[T, Hkv, D] bf16 into the slots slot_map[T] (i64, page * 128 + place).  Tokens with a negative slot are left out; so are those with a
+ * slot beyond the pool, which set *status (device word, nullable) to SPECROLL_ELIMIT.  Nothing but the slots' own bytes is written.
+ * The slots of one call must differ: of two tokens for one slot, either's bytes may stay. */
+int specroll_kv4_store(int64_t T, int32_t Hkv, int32_t D, const void *K, const void *V, const int64_t *slot_map, void *pool,
+                       int64_t n_pages, int32_t *status, void *cuda_stream);
+
+/* The values at the slots slot_map[T] back as bf16 K, V[T, Hkv, D] (exactly; a slot may occur more than once): a cached prefix for
+ * kernels that read bf16, or a cache on its way out.  Zeros for slots that are negative or beyond the pool; *status as above. */
+int specroll_kv4_load(int64_t T, int32_t Hkv, int32_t D, const void *pool, int64_t n_pages, const int64_t *slot_map, void *K,
+                      void *V, int32_t *status, void *cuda_stream);
+
+/* specroll_commit_path and specroll_commit_path_layers for pools in 4 bits (pool: one per layer in the place of Kp and Vp); everything
+ * else as there. */
+int specroll_commit_path_kv4(int32_t B, int32_t N, int32_t K, int32_t Hkv, int32_t D, const void *Kt, const void *Vt,
+                             const int32_t *path_node, const int32_t *n_acc, void *pool, int64_t n_pages,
+                             const int32_t *page_table, const int32_t *page_indptr, const int32_t *kv_len,
+                             int32_t *kv_len_out, int32_t *status, void *cuda_stream);
+
+int specroll_commit_path_kv4_layers(int32_t B, int32_t N, int32_t K, int32_t Hkv, int32_t D, int32_t n_layers,
+                                    const void *const *Kt, const void *const *Vt, const int32_t *path_node,
+                                    const int32_t *n_acc, void *const *pool, int64_t n_pages, const int32_t *page_table,
+                                    const int32_t *page_indptr, const int32_t *kv_len, int32_t *kv_len_out,
+                                    int32_t *status, void *cuda_stream);
+
+/* specroll_tree_attn_paged over such a pool: exactly the attention of the cached values as decoded and of the tree's bf16 rows Kt, Vt
+ * (scores and sums in fp32, probabilities rounded to bf16 for the product with V, as there).  N = 1 with parent {-1} is plain decoding of one
+ * token a sequence, whose own K and V are Kt and Vt.  Tree rows that a node does not see are multiplied by a zero weight: they must hold
+ * finite values.  Pages outside [0, n_pages) read as zeros.  Flags, plan and workspace as for specroll_tree_attn_paged. */
+size_t specroll_tree_attn_kv4_workspace_bytes(const specroll_attn_desc *desc, const int32_t *kv_len_host);
+
+int specroll_tree_attn_kv4(const specroll_attn_desc *desc, const void *Q, const void *pool, int64_t n_pages,
+                           const int32_t *page_table_dev, const int32_t *page_indptr_dev, const int32_t *kv_len_dev,
+                           const int32_t *kv_len_host, const void *Kt, const void *Vt, const int32_t *parent_host, void *O,
+                           float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
  * Verifier-derived feedback of matured proposals and the trajectory memory update (Sec. 3.3 Eq.
  * "acceptance-gap-decomposition"; Sec. 3.4 Eq. "support", "distdir", "covdir", "unified-feedback",
  * "ema").  It produces the memory m that specroll_propose consumes.  Per record r (one matured

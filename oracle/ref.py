@@ -483,3 +483,116 @@ def target_head(H, W, temperature=1.0, want_id=None):
         out["want_logit"] = np.take_along_axis(bits, np.asarray(want_id, np.int64), -1)
     return out
 
+
+
+# ------------------------------------------------------------------ paged cache in 4 bits, page tables
+
+KV4_STEPS = np.array([(8 + c % 8) * 2.0 ** (c // 8 - 23) for c in range(256)])   # what a scale byte stands for
+
+
+def kv4_quantise(x):
+    """Codes q (int8, x's shape) and scale bytes (uint8, one for 32 elements) of float64 values x [..., D]: the scale is the one
+    nearest to the largest magnitude over 7 (the larger of two), the code the nearest whole multiple (halves away from zero)."""
+    x = np.asarray(x, np.float64)
+    x = np.where(np.isnan(x), 0.0, x).reshape(x.shape[:-1] + (-1, 32))
+    top = np.abs(x).max(-1)
+    borders = 7 * (KV4_STEPS[1:] + KV4_STEPS[:-1]) / 2
+    c = np.searchsorted(borders, top, side="right")
+    t = x / KV4_STEPS[c][..., None]
+    q = np.clip(np.trunc(np.clip(t, -9, 9) + np.copysign(0.5, t)), -8, 7)
+    return q.astype(np.int8).reshape(x.shape[:-2] + (-1,)), c.astype(np.uint8)
+
+
+def kv4_values(q, c):
+    return np.asarray(q, np.float64) * np.repeat(KV4_STEPS[np.asarray(c)], 32, axis=-1)
+
+
+def kv4_pack(q, c):
+    """Tiles uint8 [..., tile] of a page's codes [..., 128, D] and scale bytes [..., 128, D/32]."""
+    n = (np.asarray(q, np.int64) + 8).reshape(q.shape[:-1] + (-1, 8))
+    word = np.zeros(n.shape[:-1], np.int64)
+    for e in range(8):
+        word |= n[..., e] << (4 * (e // 2) + 16 * (e % 2))
+    codes = word.astype("<u4").view(np.uint8)
+    lead = q.shape[:-2]
+    return np.concatenate([codes.reshape(lead + (-1,)), np.asarray(c, np.uint8).reshape(lead + (-1,))], -1)
+
+
+def kv4_unpack(tile, D):
+    """Codes [..., 128, D] and scale bytes [..., 128, D/32] of tiles."""
+    lead = tile.shape[:-1]
+    word = np.ascontiguousarray(tile[..., :64 * D]).view("<u4").reshape(lead + (128, D // 8))
+    q = np.stack([((word >> (4 * (e // 2) + 16 * (e % 2))) & 15).astype(np.int8) - 8 for e in range(8)], -1)
+    return q.reshape(lead + (128, D)), tile[..., 64 * D:].reshape(lead + (128, D // 32))
+
+
+def kv4_pool_values(pool, D):
+    """K, V float64 [n_pages, 128, Hkv, D] of a pool uint8 [n_pages, Hkv, 2, tile]."""
+    v = kv4_values(*kv4_unpack(pool, D))
+    return v[:, :, 0].transpose(0, 2, 1, 3), v[:, :, 1].transpose(0, 2, 1, 3)
+
+
+def kv4_store(K, V, slots, pool):
+    """The pool after K, V [T, Hkv, D] (float64) have gone to their slots."""
+    pool, D = pool.copy(), K.shape[-1]
+    for kv, x in ((0, K), (1, V)):
+        q, c = kv4_quantise(x)
+        for t, slot in enumerate(slots):
+            if 0 <= slot < 128 * pool.shape[0]:
+                page, at = divmod(int(slot), 128)
+                for h in range(x.shape[1]):
+                    row = kv4_pack(np.broadcast_to(q[t, h], (128, D)), np.broadcast_to(c[t, h], (128, D // 32)))
+                    pool[page, h, kv, at * D // 2:(at + 1) * D // 2] = row[:D // 2]
+                    at_s = 64 * D + at * (D // 32)
+                    pool[page, h, kv, at_s:at_s + D // 32] = row[64 * D:64 * D + D // 32]
+    return pool
+
+
+def tree_attn64(Q, K, V, kv_len, Kt, Vt, parent, scale):
+    """Attention in float64 over caches given as lists of [L_b, Hkv, D].  Returns O, lse, and the sum of p |v| (what a rounding
+    of p is relative to) and the largest sum of |q k| scale."""
+    B, N, Hq, D = Q.shape
+    Hkv = Kt.shape[2]
+    anc = np.eye(N, dtype=bool)
+    for n in range(1, N):
+        anc[n] |= anc[parent[n]]
+    O, A, lse, dot = np.zeros(Q.shape), np.zeros(Q.shape), np.zeros((B, N, Hq)), 0.0
+    for b in range(B):
+        L = int(kv_len[b])
+        may = np.concatenate([np.ones((N, L), bool), anc], 1)
+        for h in range(Hq):
+            g = h // (Hq // Hkv)
+            k, v = np.concatenate([K[b][:, g], Kt[b, :, g]]), np.concatenate([V[b][:, g], Vt[b, :, g]])
+            s = np.where(may, Q[b, :, h] @ k.T * scale, -np.inf)
+            dot = max(dot, float((np.abs(Q[b, :, h]) @ np.abs(k).T).max() * scale))
+            m = s.max(1, keepdims=True)
+            p = np.exp(s - m)
+            l = p.sum(1, keepdims=True)
+            O[b, :, h], A[b, :, h], lse[b, :, h] = p @ v / l, p @ np.abs(v) / l, (m + np.log(l))[:, 0]
+    return O, lse, A, dot
+
+
+def page_plan(kv_len, add, page_table, page_indptr, free_list, n_free, table_cap, slot_cap):
+    """Page tables, slots and the free list, sequence by sequence."""
+    free, given, table, indptr, tok, slots, short = [int(p) for p in free_list[:n_free]], [], [], [0], [0], [], False
+    for b in range(len(kv_len)):
+        pages = [int(p) for p in page_table[page_indptr[b]:page_indptr[b + 1]]]
+        if add[b] < 0:
+            given += pages
+            pages = []
+        L = max(0, int(kv_len[b]))
+        while add[b] >= 0 and len(pages) * 128 < L + add[b]:
+            short |= not free
+            pages.append(free.pop(0) if free else -1)
+        for i in range(max(0, int(add[b]))):
+            page = pages[(L + i) // 128]
+            slots.append(page * 128 + (L + i) % 128 if page >= 0 else -1)
+        table += pages
+        indptr.append(len(table))
+        tok.append(len(slots))
+    free += given
+    short |= len(table) > table_cap or len(slots) > slot_cap or len(free) > len(free_list)
+    fit = lambda v, n, dt: np.array((v + [-1] * n)[:n], dt)  # noqa: E731
+    return dict(page_table=fit(table, table_cap, np.int32), page_indptr=np.array(indptr, np.int32), tok_indptr=np.array(tok, np.int32),
+                slot_map=fit(slots, slot_cap, np.int64), free_list=fit(free, len(free_list), np.int32),
+                n_free=min(len(free), len(free_list)), short=short)

@@ -34,6 +34,8 @@ EXPORTS = ("specroll_version", "specroll_strerror", "specroll_node_budget", "spe
            "specroll_reflex_sketch", "specroll_reflex_gate",
            "specroll_target_head_stats_workspace_bytes", "specroll_target_head_stats", "specroll_target_head_rows",
            "specroll_verify_want_ids", "specroll_verify_walk_sparse", "specroll_verify_terminal_rows",
+           "specroll_page_plan", "specroll_kv4_tile_bytes", "specroll_kv4_store", "specroll_kv4_load", "specroll_commit_path_kv4",
+           "specroll_commit_path_kv4_layers", "specroll_tree_attn_kv4_workspace_bytes", "specroll_tree_attn_kv4",
            "specroll_target_head_tile_mass_bytes", "specroll_target_head_stats_tiles", "specroll_verify_hidden")
 
 
@@ -96,12 +98,14 @@ def lib():
         for n in ("specroll_propose_workspace_bytes", "specroll_verify_workspace_bytes",
                   "specroll_tree_attn_workspace_bytes", "specroll_tree_attn_paged_workspace_bytes",
                   "specroll_verify_nucleus_workspace_bytes", "specroll_reflex_feedback_workspace_bytes",
-                  "specroll_target_head_stats_workspace_bytes"):
+                  "specroll_target_head_stats_workspace_bytes", "specroll_kv4_tile_bytes",
+                  "specroll_tree_attn_kv4_workspace_bytes"):
             getattr(l, n).restype = C.c_size_t
         for n in ("specroll_propose", "specroll_workspace_status", "specroll_tree_draw", "specroll_tree_attn",
                   "specroll_verify", "specroll_verify_static", "specroll_tree_attn_paged", "specroll_commit_path",
                   "specroll_commit_path_layers", "specroll_gather_hidden", "specroll_verify_nucleus",
-                  "specroll_tree_attn_launches", "specroll_reflex_feedback"):
+                  "specroll_tree_attn_launches", "specroll_reflex_feedback", "specroll_page_plan", "specroll_kv4_store",
+                  "specroll_kv4_load", "specroll_commit_path_kv4", "specroll_commit_path_kv4_layers", "specroll_tree_attn_kv4"):
             getattr(l, n).restype = C.c_int
         try:
             from . import _native as n
@@ -145,7 +149,7 @@ def _stream() -> C.c_void_p:
 _empty = torch.empty
 
 
-_DTYPES = {0: torch.uint8, 3: torch.int32, 6: torch.float32, 15: torch.bfloat16}   # by at::ScalarType
+_DTYPES = {0: torch.uint8, 3: torch.int32, 4: torch.int64, 6: torch.float32, 15: torch.bfloat16}   # by at::ScalarType
 
 
 def _alloc_for_native(shape, dtype_code, device_index):
@@ -273,6 +277,60 @@ def commit_path_layers(Kt, Vt, path_node, n_acc, Kp, Vp, page_table, page_indptr
 def gather_hidden(hidden, term_node, out=None):
     """specroll_gather_hidden: hidden[B,N,d] bf16, term_node[B] -> h_next[B,d]."""
     return _n().gather_hidden(hidden, term_node, out)
+
+
+# ----------------------------------------------------------------------------------- paged cache in 4 bits
+
+
+def page_plan(kv_len, add, page_table, page_indptr, free_list, n_free, table_cap, slot_cap, status=None,
+              out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """specroll_page_plan: page tables, the slots of add[b] new tokens a sequence, and the free list afterwards (all device
+    int32, slot_map int64).  ``table_cap``: entries of the new table; ``slot_cap``: new tokens (sum of the positive add).
+    Returns page_table [table_cap], page_indptr [B+1], tok_indptr [B+1], slot_map [slot_cap], free_list (as long as the given
+    one), n_free [1]."""
+    return _n().page_plan(kv_len, add, page_table, page_indptr, free_list, n_free, table_cap, slot_cap, status, out)
+
+
+def kv4_tile_bytes(D) -> int:
+    """Bytes of a page's K or V of one head; a layer's pool is uint8 [n_pages, Hkv, 2, kv4_tile_bytes(D)]."""
+    return int(lib().specroll_kv4_tile_bytes(C.c_int32(D)))
+
+
+def kv4_store(K, V, slot_map, pool, status=None):
+    """specroll_kv4_store: K, V [T, Hkv, D] bf16 into the slots slot_map [T] int64 of a 4-bit pool (in place)."""
+    _n().kv4_store(K, V, slot_map, pool, status)
+
+
+def kv4_load(pool, slot_map, out=None, status=None):
+    """specroll_kv4_load: the values at slot_map [T] int64 as bf16 (K, V), [T, Hkv, D] each.  ``out``: a pair of tensors for them."""
+    return _n().kv4_load(pool, slot_map, out, status)
+
+
+def commit_path_kv4(Kt, Vt, path_node, n_acc, pool, page_table, page_indptr, kv_len, kv_len_out=None, status=None):
+    """specroll_commit_path_kv4: appends the committed path's tree rows to one layer's 4-bit paged cache (in place)."""
+    _n().commit_path_kv4_layers((Kt,), (Vt,), path_node, n_acc, (pool,), page_table, page_indptr, kv_len, kv_len_out, status)
+
+
+def commit_path_kv4_layers(Kt, Vt, path_node, n_acc, pool, page_table, page_indptr, kv_len, kv_len_out=None, status=None):
+    """specroll_commit_path_kv4_layers: Kt, Vt, pool are lists with one tensor per layer."""
+    _n().commit_path_kv4_layers(Kt, Vt, path_node, n_acc, pool, page_table, page_indptr, kv_len, kv_len_out, status)
+
+
+def tree_attn_kv4_workspace_bytes(B, N, Hq, Hkv, D, kv_len_host, scale=None) -> int:
+    kl = _host_i32(kv_len_host, "kv_len_host")
+    desc = AttnDesc(B, N, Hq, Hkv, D, scale if scale is not None else 1.0 / float(np.sqrt(D)), 0)
+    return int(lib().specroll_tree_attn_kv4_workspace_bytes(C.byref(desc), kl.ctypes.data_as(C.c_void_p)))
+
+
+def tree_attn_kv4(Q, pool, page_table, page_indptr, kv_len_dev, kv_len_host, Kt, Vt, parent, scale=None, want_lse=False,
+                  workspace=None, out=None, lse=None, flags: int = 0, check_status: bool = False):
+    """specroll_tree_attn_kv4.  pool: uint8 [n_pages, Hkv, 2, kv4_tile_bytes(D)]; the other arguments as for
+    ``tree_attn_paged``.  Returns O (and lse when asked)."""
+    out, lse, workspace = _n().tree_attn_kv4(Q, pool, page_table, page_indptr, kv_len_dev, kv_len_host, Kt, Vt, parent, scale,
+                                             want_lse, workspace, out, lse, flags)
+    if check_status:
+        _check(workspace_status(workspace), "specroll_workspace_status")
+    return (out, lse) if want_lse else out
 
 
 # ----------------------------------------------------------------------------------- verify

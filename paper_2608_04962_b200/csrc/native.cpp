@@ -28,7 +28,7 @@ PyObject *g_error = nullptr;     // SpecrollError
 PyObject *g_host_i32 = nullptr;  // binding._host_i32: anything array-like -> contiguous int32 numpy array
 PyObject *g_alloc = nullptr;     // replacement of torch.empty as f(shape, dtype code, device index), or nullptr
 
-constexpr at::ScalarType BF16 = at::kBFloat16, F32 = at::kFloat, I32 = at::kInt, U8 = at::kByte;
+constexpr at::ScalarType BF16 = at::kBFloat16, F32 = at::kFloat, I32 = at::kInt, I64 = at::kLong, U8 = at::kByte;
 
 [[noreturn]] void fail(const char *fmt, ...) {
     va_list ap;
@@ -53,7 +53,9 @@ constexpr at::ScalarType BF16 = at::kBFloat16, F32 = at::kFloat, I32 = at::kInt,
     X(specroll_reflex_sketch) X(specroll_reflex_gate) X(specroll_target_head_stats_workspace_bytes)                  \
     X(specroll_target_head_stats) X(specroll_target_head_rows) X(specroll_verify_want_ids)                           \
     X(specroll_target_head_tile_mass_bytes)                                                                          \
-    X(specroll_target_head_stats_tiles) X(specroll_verify_hidden)
+    X(specroll_target_head_stats_tiles) X(specroll_verify_hidden)                                                    \
+    X(specroll_page_plan) X(specroll_kv4_tile_bytes) X(specroll_kv4_store) X(specroll_kv4_load)                      \
+    X(specroll_commit_path_kv4_layers) X(specroll_tree_attn_kv4_workspace_bytes) X(specroll_tree_attn_kv4)
 struct Entries {
 #define X(name) decltype(&::name) name;
     SPECROLL_ENTRIES(X)
@@ -335,6 +337,150 @@ PyObject *tree_attn_paged(PyObject *const *a) {
     auto *pl = lse.defined() ? (float *)dev(lse, F32, "lse") : nullptr;
     CALL(specroll_tree_attn_paged, &desc, pq, pk, pv, (int64_t)Kp.size(0), pt, pip, pkl, len.data(), pkt, pvt, parent.data(), po, pl, ptr(ws), bytes_of(ws));
     return attn_result(O, lse, ws);
+}
+
+// A 4-bit pool [n_pages, Hkv, 2, tile]; returns D by its tile.
+int64_t kv4_dim(const at::Tensor &pool, const char *what) {
+    for (const int32_t D : {64, 128})
+        if (pool.dim() == 4 && pool.size(2) == 2 && pool.size(3) == (int64_t)lib.specroll_kv4_tile_bytes(D)) return D;
+    fail("%s: the pool must be [n_pages, Hkv, 2, kv4_tile_bytes(D)]", what);
+}
+
+PyObject *tree_attn_kv4(PyObject *const *a) {
+    // Q, pool, page_table, page_indptr, kv_len_dev, kv_len_host, Kt, Vt, parent, scale, want_lse, workspace, out, lse, flags
+    const at::Tensor &Q = need(a[0], "Q", 4), &pool = need(a[1], "pool", 4), &Kt = need(a[6], "Kt", 4), &Vt = need(a[7], "Vt", 4);
+    const at::Tensor &pi = need(a[3], "page_indptr"), &kl = need(a[4], "kv_len_dev");
+    HostI32 len(a[5], "kv_len_host"), parent(a[8], "parent");
+    const int64_t B = Q.size(0), N = Q.size(1), Hq = Q.size(2), D = Q.size(3), Hkv = Kt.size(2);
+    if (len.size() != B || !shape(Kt, {B, N, Hkv, D}) || !shape(Vt, {B, N, Hkv, D}) || parent.size() < N)
+        fail("tree_attn_kv4: inconsistent shapes");
+    if (kv4_dim(pool, "tree_attn_kv4") != D || pool.size(1) != Hkv) fail("tree_attn_kv4: the pool is for another shape of head");
+    if (pi.numel() != B + 1 || kl.numel() != B) fail("tree_attn_kv4: page_indptr / kv_len_dev sizes");
+    const specroll_attn_desc desc = {(int32_t)B, (int32_t)N, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, attn_scale(a[9], D), (int32_t)integer(a[14])};
+    const at::Tensor O = a[12] != Py_None ? need(a[12], "out", 4) : alloc({B, N, Hq, D}, BF16, Q);
+    if (!shape(O, {B, N, Hq, D})) fail("tree_attn_kv4: out must be [B, N, Hq, D]");
+    at::Tensor lse;
+    if (a[13] != Py_None) lse = need(a[13], "lse", 3);
+    else if (PyObject_IsTrue(a[10])) lse = alloc({B, N, Hq}, F32, Q);
+    if (lse.defined() && !shape(lse, {B, N, Hq})) fail("tree_attn_kv4: lse must be [B, N, Hq]");
+    const at::Tensor ws = workspace(a[11], a[11] == Py_None ? lib.specroll_tree_attn_kv4_workspace_bytes(&desc, len.data()) : 0, Q);
+    const void *pq = dev(Q, BF16, "Q"), *pp = dev(pool, U8, "pool"), *pkt = dev(Kt, BF16, "Kt"), *pvt = dev(Vt, BF16, "Vt");
+    const auto *pt = (const int32_t *)dev(a[2], I32, "page_table"), *pip = (const int32_t *)dev(pi, I32, "page_indptr"), *pkl = (const int32_t *)dev(kl, I32, "kv_len_dev");
+    void *po = dev(O, BF16, "out");
+    auto *pl = lse.defined() ? (float *)dev(lse, F32, "lse") : nullptr;
+    CALL(specroll_tree_attn_kv4, &desc, pq, pp, (int64_t)pool.size(0), pt, pip, pkl, len.data(), pkt, pvt, parent.data(), po, pl, ptr(ws), bytes_of(ws));
+    return attn_result(O, lse, ws);
+}
+
+// ------------------------------------------------------------------------------ paged cache in 4 bits, page tables
+
+PyObject *page_plan(PyObject *const *a) {
+    // kv_len, add, page_table, page_indptr, free_list, n_free, table_cap, slot_cap, status, out
+    const at::Tensor &kl = need(a[0], "kv_len", 1), &add = need(a[1], "add", 1), &pt = need(a[2], "page_table", 1), &pi = need(a[3], "page_indptr", 1);
+    const at::Tensor &fl = need(a[4], "free_list", 1), &nf = need(a[5], "n_free");
+    const int64_t B = kl.numel(), table_cap = integer(a[6]), slot_cap = integer(a[7]);
+    if (add.numel() != B || pi.numel() != B + 1 || nf.numel() != 1) fail("page_plan: inconsistent shapes");
+    if (table_cap < 0 || slot_cap < 0 || table_cap > INT32_MAX || pt.numel() > INT32_MAX || fl.numel() > INT32_MAX || B > INT32_MAX)
+        fail("page_plan: sizes out of range");
+    const at::Tensor *st = tensor(a[8], "status");
+    if (st && st->numel() != 1) fail("page_plan: status must be one word");
+    const auto *pl = (const int32_t *)dev(kl, I32, "kv_len"), *pa = (const int32_t *)dev(add, I32, "add"), *ppt = (const int32_t *)dev(pt, I32, "page_table");
+    const auto *ppi = (const int32_t *)dev(pi, I32, "page_indptr"), *pf = (const int32_t *)dev(fl, I32, "free_list"), *pn = (const int32_t *)dev(nf, I32, "n_free");
+    auto *ps = (int32_t *)dev(st, I32, "status");
+    if (a[9] != Py_None) {
+        const struct { const char *name; int64_t n; } want[] = {{"page_table", table_cap}, {"page_indptr", B + 1}, {"tok_indptr", B + 1},
+                                                                {"slot_map", slot_cap}, {"free_list", fl.numel()}, {"n_free", 1}};
+        for (const auto &w : want) {
+            const Ref o(PyMapping_GetItemString(a[9], w.name));
+            if (need(o.o, w.name).numel() != w.n) fail("page_plan: out[%s] must have %lld entries", w.name, (long long)w.n);
+        }
+    }
+    Out out(a[9]);
+    auto *ot = (int32_t *)out.get("page_table", {table_cap}, I32, kl);
+    auto *oi = (int32_t *)out.get("page_indptr", {B + 1}, I32, kl);
+    auto *ok = (int32_t *)out.get("tok_indptr", {B + 1}, I32, kl);
+    auto *os = (int64_t *)out.get("slot_map", {slot_cap}, I64, kl);
+    auto *of = (int32_t *)out.get("free_list", {fl.numel()}, I32, kl);
+    auto *on = (int32_t *)out.get("n_free", {1}, I32, kl);
+    CALL(specroll_page_plan, (int32_t)B, pl, pa, ppt, (int32_t)pt.numel(), ppi, pf, (int32_t)fl.numel(), pn, (int32_t)table_cap, slot_cap, ot, oi, ok, os, of,
+         on, ps);
+    return out.release();
+}
+
+PyObject *kv4_store(PyObject *const *a) {
+    // K, V, slot_map, pool, status
+    const at::Tensor &K = need(a[0], "K", 3), &V = need(a[1], "V", 3), &slots = need(a[2], "slot_map", 1), &pool = need(a[3], "pool", 4);
+    const int64_t T = K.size(0), Hkv = K.size(1), D = K.size(2);
+    if (V.sizes() != K.sizes() || slots.numel() != T) fail("kv4_store: inconsistent shapes");
+    if (kv4_dim(pool, "kv4_store") != D || pool.size(1) != Hkv) fail("kv4_store: the pool is for another shape of head");
+    const at::Tensor *st = tensor(a[4], "status");
+    if (st && st->numel() != 1) fail("kv4_store: status must be one word");
+    const void *pk = dev(K, BF16, "K"), *pv = dev(V, BF16, "V");
+    const auto *ps = (const int64_t *)dev(slots, I64, "slot_map");
+    void *pp = dev(pool, U8, "pool");
+    auto *pw = (int32_t *)dev(st, I32, "status");
+    CALL(specroll_kv4_store, T, (int32_t)Hkv, (int32_t)D, pk, pv, ps, pp, (int64_t)pool.size(0), pw);
+    return Py_NewRef(Py_None);
+}
+
+PyObject *kv4_load(PyObject *const *a) {
+    // pool, slot_map, out, status
+    const at::Tensor &pool = need(a[0], "pool", 4), &slots = need(a[1], "slot_map", 1);
+    const int64_t T = slots.numel(), Hkv = pool.size(1), D = kv4_dim(pool, "kv4_load");
+    at::Tensor kv[2];
+    if (a[2] != Py_None) {
+        const Ref pair(PySequence_Fast(a[2], "kv4_load: out must be a pair of tensors"));
+        if (PySequence_Fast_GET_SIZE(pair.o) != 2) fail("kv4_load: out must be a pair of tensors");
+        for (int i = 0; i < 2; ++i) {
+            kv[i] = need(PySequence_Fast_GET_ITEM(pair.o, i), "out", 3);
+            if (!shape(kv[i], {T, Hkv, D})) fail("kv4_load: out must be [T, Hkv, D]");
+        }
+    } else {
+        for (auto &t : kv) t = alloc({T, Hkv, D}, BF16, pool);
+    }
+    const at::Tensor *st = tensor(a[3], "status");
+    if (st && st->numel() != 1) fail("kv4_load: status must be one word");
+    const void *pp = dev(pool, U8, "pool");
+    const auto *ps = (const int64_t *)dev(slots, I64, "slot_map");
+    void *pk = dev(kv[0], BF16, "out"), *pv = dev(kv[1], BF16, "out");
+    auto *pw = (int32_t *)dev(st, I32, "status");
+    CALL(specroll_kv4_load, T, (int32_t)Hkv, (int32_t)D, pp, (int64_t)pool.size(0), ps, pk, pv, pw);
+    return Py_BuildValue("NN", THPVariable_Wrap(kv[0]), THPVariable_Wrap(kv[1]));
+}
+
+PyObject *commit_path_kv4_layers(PyObject *const *a) {
+    // three sequences of tensors, one per layer; Kt, Vt, path_node, n_acc, pool, page_table, page_indptr, kv_len, kv_len_out, status
+    static const char *const names[3] = {"Kt", "Vt", "pool"};
+    PyObject *const src[3] = {a[0], a[1], a[4]};
+    std::vector<Ref> seqs;
+    std::vector<void *> ptrs[3];
+    const at::Tensor *first[3] = {nullptr, nullptr, nullptr};
+    Py_ssize_t n = 0;
+    for (int i = 0; i < 3; ++i) {
+        seqs.emplace_back(PySequence_Fast(src[i], "commit_path_kv4_layers: one tensor per layer in each list"));
+        const Py_ssize_t len = PySequence_Fast_GET_SIZE(seqs.back().o);
+        if (i == 0) n = len;
+        if (len != n || n == 0) fail("commit_path_kv4_layers: one tensor per layer in each list");
+        for (Py_ssize_t l = 0; l < n; ++l) {
+            const at::Tensor &t = need(PySequence_Fast_GET_ITEM(seqs.back().o, l), names[i], 4);
+            if (!first[i]) first[i] = &t;
+            if (i < 2 ? t.sizes() != first[0]->sizes() : t.sizes() != first[2]->sizes())
+                fail("commit_path_kv4_layers: %s differs in shape between layers", names[i]);
+            ptrs[i].push_back(dev(t, i < 2 ? BF16 : U8, names[i]));
+        }
+    }
+    const at::Tensor &Kt = *first[0], &pool = *first[2], &path = need(a[2], "path_node", 2);
+    const int64_t B = Kt.size(0), N = Kt.size(1), Hkv = Kt.size(2), D = Kt.size(3), K = path.size(1) - 1;
+    if (kv4_dim(pool, "commit_path_kv4_layers") != D || pool.size(1) != Hkv) fail("commit_path_kv4_layers: the pool is for another shape of head");
+    const at::Tensor &na = need(a[3], "n_acc"), &pi = need(a[6], "page_indptr"), &kl = need(a[7], "kv_len"), *ko = tensor(a[8], "kv_len_out"), *st = tensor(a[9], "status");
+    if (path.size(0) != B || na.numel() != B || pi.numel() != B + 1 || kl.numel() != B || (ko && ko->numel() != B) || (st && st->numel() != 1))
+        fail("commit_path_kv4_layers: inconsistent shapes");
+    const auto *pp = (const int32_t *)dev(path, I32, "path_node"), *pn = (const int32_t *)dev(na, I32, "n_acc");
+    const auto *pt = (const int32_t *)dev(a[5], I32, "page_table"), *ppi = (const int32_t *)dev(pi, I32, "page_indptr"), *pl = (const int32_t *)dev(kl, I32, "kv_len");
+    auto *po = (int32_t *)dev(ko, I32, "kv_len_out"), *ps = (int32_t *)dev(st, I32, "status");
+    CALL(specroll_commit_path_kv4_layers, (int32_t)B, (int32_t)N, (int32_t)K, (int32_t)Hkv, (int32_t)D, (int32_t)n, ptrs[0].data(), ptrs[1].data(), pp, pn,
+         ptrs[2].data(), (int64_t)pool.size(0), pt, ppi, pl, po, ps);
+    return Py_NewRef(Py_None);
 }
 
 // ------------------------------------------------------------------------------ between two rounds
@@ -659,6 +805,11 @@ PyMethodDef methods[] = {METHOD(attach, 3),
                          METHOD(tree_draw, 6),
                          METHOD(tree_attn, 14),
                          METHOD(tree_attn_paged, 16),
+                         METHOD(tree_attn_kv4, 15),
+                         METHOD(page_plan, 10),
+                         METHOD(kv4_store, 5),
+                         METHOD(kv4_load, 4),
+                         METHOD(commit_path_kv4_layers, 10),
                          METHOD(commit_path, 11),
                          METHOD(commit_path_layers, 11),
                          METHOD(gather_hidden, 3),

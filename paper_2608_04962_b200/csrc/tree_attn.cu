@@ -535,7 +535,7 @@ static bool merge_by_kernel(long long units, int max_ns) { return max_ns >= 5 ||
 // the order the device uses, to whichever of PLAN_SMS CTAs is free first.  A unit costs its K/V tiles, one more for the
 // tree tile of a sequence's last chunk, one for the hand-over between units; a chunk of a split sequence adds one
 // for its partial, and the last one the merge when the attention kernel does it, else the merge kernel follows.
-static long long estimate_makespan(const std::vector<int> &tiles, int ct, int copies) {
+static long long estimate_makespan(const std::vector<int> &tiles, int ct, int copies, int places = PLAN_SMS) {
     struct Chunk { int tps, cost; };
     std::vector<Chunk> chunks;
     int max_ns = 1;
@@ -553,7 +553,7 @@ static long long estimate_makespan(const std::vector<int> &tiles, int ct, int co
     }
     std::stable_sort(chunks.begin(), chunks.end(), [](const Chunk &x, const Chunk &y) { return x.tps > y.tps; });
     std::priority_queue<long long, std::vector<long long>, std::greater<long long>> sms;
-    for (int i = 0; i < PLAN_SMS; ++i) sms.push(0);
+    for (int i = 0; i < places; ++i) sms.push(0);
     long long end = 0;
     for (const Chunk &c : chunks)
         for (int k = 0; k < copies; ++k) {
@@ -570,10 +570,11 @@ struct AttnPlan {
     int max_splits;  // chunks of the longest sequence
     int merge_mode;  // tcgen05 path: 0 = split sequences are merged inside the attention kernel, 2 = by a kernel after it
     bool use_tc;
+    bool kv4;        // 4-bit cache
     size_t off_status, off_items, off_sorted, off_rank, off_tab, off_counters, off_po, off_pml, off_hand, total;
 };
 
-static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_host, AttnPlan *p) {
+static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_host, bool kv4, AttnPlan *p) {
     if (!d || !indptr_host || d->B < 0 || d->N < 1 || d->N > SPECROLL_MAX_NODES || d->Hq < 1 || d->Hkv < 1 ||
         (d->Hq % d->Hkv) || (d->D != 64 && d->D != 128) || (d->flags & ~SPECROLL_ATTN_ALL_FLAGS) != 0 ||
         !(d->scale > 0.f))
@@ -584,7 +585,15 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     p->tile_tokens = p->use_tc ? 128 : AT_BN;  // KV tokens per tile of the chosen kernel
     const int TT = p->tile_tokens;
     p->rows = d->N * G;
-    if (p->use_tc) {
+    p->kv4 = kv4;
+    int places = PLAN_SMS;  // CTAs that run side by side
+    if (kv4) {
+        // 8 or 16 rows a CTA, which need not be whole nodes
+        p->rows_per_block = p->rows <= 8 ? 8 : 16;
+        p->n_rb = (p->rows + p->rows_per_block - 1) / p->rows_per_block;
+        p->nodes_per_block = 0;
+        if (p->rows_per_block == 8) places = 2 * PLAN_SMS;
+    } else if (p->use_tc) {
         // row blocks are whole nodes: (node, head-in-group) rows of a block are one TMA box
         // The softmax of a row block costs the same whether the block is full or not, so the rows go into as
         // few blocks as possible.  Every block is a work unit of its own; the units of one (chunk, KV head)
@@ -621,7 +630,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     // so that the fp32 partials stay a small fraction of the KV bytes.
     const long long ctas_per_tile = (long long)d->Hkv * p->n_rb;
     auto chunk_for = [&](int per_sm_pct) -> int {
-        long long c = (tiles_total * ctas_per_tile * 100 + (long long)PLAN_SMS * per_sm_pct - 1) / ((long long)PLAN_SMS * per_sm_pct);
+        long long c = (tiles_total * ctas_per_tile * 100 + (long long)places * per_sm_pct - 1) / ((long long)places * per_sm_pct);
         if (c < 512 / TT) c = 512 / TT;
         if (c > max_tiles) c = max_tiles > 0 ? max_tiles : 1;
         return (int)c;
@@ -638,7 +647,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
             for (int i = 0; i < n_seen; ++i)
                 if (seen[i] == c) return;
             seen[n_seen++] = c;
-            const long long m = estimate_makespan(tiles, c, (int)ctas_per_tile);
+            const long long m = estimate_makespan(tiles, c, (int)ctas_per_tile, places);
             if (best < 0 || m < best) {
                 best = m;
                 ct = c;
@@ -665,6 +674,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     if (max_tiles / p->chunk_tiles + 1 > 65535) return SPECROLL_EINVAL;
     p->max_splits = (max_tiles + p->chunk_tiles - 1) / p->chunk_tiles;
     p->merge_mode = (p->use_tc && merge_by_kernel((long long)items * ctas_per_tile, (max_tiles + p->chunk_tiles - 1) / p->chunk_tiles)) ? 2 : 0;
+    if (kv4) p->merge_mode = 2;  // (its CTAs leave when their chunk is done)
     if (p->use_tc && items == d->B) p->merge_mode = 2;  // (nothing is split: nothing is merged anywhere)
     p->n_counters = 64 + d->B * d->Hkv * p->n_rb;  // [0]: work counter, [1]: CTAs that have left; [64 ...]: per (b, hkv, rb) arrivals
     size_t o = 0;
@@ -709,7 +719,7 @@ static int launch_attn(const AttnArgs &a, const TopoMask &mask, const AttnPlan &
 using namespace specroll;
 
 // Plans are remembered for the last few (shape, lengths) seen: every layer of a step asks for the same one.
-static int make_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_host, AttnPlan *p) {
+static int make_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_host, AttnPlan *p, bool kv4 = false) {
     struct Entry {
         int key[7];
         std::vector<int32_t> indptr;
@@ -718,10 +728,10 @@ static int make_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_hos
     static std::mutex mu;
     static Entry cache[4];
     static unsigned next = 0;
-    if (!d || !indptr_host || d->B < 0 || d->B > (1 << 24)) return compute_attn_plan(d, indptr_host, p);
+    if (!d || !indptr_host || d->B < 0 || d->B > (1 << 24)) return compute_attn_plan(d, indptr_host, kv4, p);
     // what the key leaves out is checked here, so that a remembered plan never answers for an invalid call
     if ((d->flags & ~SPECROLL_ATTN_ALL_FLAGS) != 0 || !(d->scale > 0.f)) return SPECROLL_EINVAL;
-    const int key[7] = {d->B, d->N, d->Hq, d->Hkv, d->D, (int)(d->flags & SPECROLL_ATTN_LEGACY_MMA), 1};
+    const int key[7] = {d->B, d->N, d->Hq, d->Hkv, d->D, (int)(d->flags & SPECROLL_ATTN_LEGACY_MMA), kv4 ? 2 : 1};
     const size_t n = (size_t)d->B + 1;
     std::lock_guard<std::mutex> lock(mu);
     for (Entry &e : cache)
@@ -730,7 +740,7 @@ static int make_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_hos
             *p = e.plan;
             return SPECROLL_OK;
         }
-    const int rc = compute_attn_plan(d, indptr_host, p);
+    const int rc = compute_attn_plan(d, indptr_host, kv4, p);
     if (rc != SPECROLL_OK) return rc;
     Entry &e = cache[next++ % 4];
     memcpy(e.key, key, sizeof(key));
@@ -756,16 +766,16 @@ extern "C" int specroll_tree_attn_launches(const specroll_attn_desc *d, const in
 }
 
 // Common body of the two entry points.  Contiguous cache: kv_indptr_dev, T_kv = cached tokens.  Paged cache:
-// kv_len_dev, page_indptr_dev, page_table_dev, T_kv = tokens in the page pool.  indptr_host is the (derived)
-// prefix of the host lengths either way.
+// kv_len_dev, page_indptr_dev, page_table_dev, T_kv = tokens in the page pool; a 4-bit one: pool4 in the place of Kc and Vc.
+// indptr_host is the (derived) prefix of the host lengths either way.
 static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void *Kc, const void *Vc, long long T_kv,
                          const int32_t *kv_indptr_dev, const int32_t *kv_len_dev, const int32_t *page_indptr_dev,
                          const int32_t *page_table_dev, const int32_t *indptr_host, const void *Kt, const void *Vt,
                          const int32_t *parent_host, void *O, float *lse, void *workspace, size_t workspace_bytes,
-                         void *cuda_stream) {
+                         void *cuda_stream, bool kv4 = false, const void *pool4 = nullptr) {
     const bool paged = page_table_dev != nullptr;
     AttnPlan p;
-    if (make_attn_plan(d, indptr_host, &p) != SPECROLL_OK) return SPECROLL_EINVAL;
+    if (make_attn_plan(d, indptr_host, &p, kv4) != SPECROLL_OK) return SPECROLL_EINVAL;
     if (d->B == 0) {  // (an empty batch has empty arrays: their pointers may be NULL)
         Topo topo0;
         TopoMask mask0;
@@ -774,11 +784,11 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     if (!Q || !Kt || !Vt || !O) return SPECROLL_EINVAL;
     if (paged ? (!kv_len_dev || !page_indptr_dev) : !kv_indptr_dev) return SPECROLL_EINVAL;
     if (paged && !p.use_tc) return SPECROLL_ELIMIT;  // the mma.sync kernel reads a contiguous cache only
-    if (T_kv > 0 && (!Kc || !Vc)) return SPECROLL_EINVAL;
+    if (T_kv > 0 && (kv4 ? !pool4 : !Kc || !Vc)) return SPECROLL_EINVAL;
     Topo topo;
     TopoMask mask;
     if (build_topo(parent_host, d->N, -1, -1, &topo, &mask) != SPECROLL_OK) return SPECROLL_EINVAL;
-    if (!aligned16(Q) || !aligned16(Kc) || !aligned16(Vc) || !aligned16(Kt) || !aligned16(Vt) || !aligned16(O))
+    if (!aligned16(Q) || !aligned16(Kc) || !aligned16(Vc) || !aligned16(Kt) || !aligned16(Vt) || !aligned16(O) || !aligned16(pool4))
         return SPECROLL_EALIGN;
     if (d->B == 0) return SPECROLL_OK;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < p.total)
@@ -824,6 +834,8 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     a.total_work = p.items * d->Hkv * p.n_rb;
     a.merge_mode = p.merge_mode;
     a.nodes_per_block = p.nodes_per_block;
+    a.pool = static_cast<const uint8_t *>(pool4);
+    a.n_pages = kv4 ? (int32_t)(T_kv / SPECROLL_PAGE_TOKENS) : 0;
     a.no_pdl = (d->flags & SPECROLL_ATTN_NO_PDL) ? 1 : 0;
     // early cache loads need a plan that is not being made by the kernel just before the attention kernel
     a.early_cache = ((d->flags & SPECROLL_ATTN_CACHE_SETTLED) && (d->flags & SPECROLL_ATTN_REUSE_PLAN)) ? 1 : 0;
@@ -838,8 +850,12 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     }
     const size_t n_out = (size_t)d->B * d->N * d->Hq;
     if (p.use_tc) {
-        const int rc = launch_attn_tc(a, mask, d->D, T_kv, status, st);
+        const int rc = p.kv4 ? launch_attn_kv4(a, mask, d->D, status, st) : launch_attn_tc(a, mask, d->D, T_kv, status, st);
         if (rc != SPECROLL_OK || p.merge_mode != 2 || p.items <= d->B) return rc;
+        if (p.kv4) {  // (the merge takes up to 128 rows a block, whatever the attention's blocks were)
+            a.n_rb = (p.rows + 127) / 128;
+            a.rows_per_block = p.rows < 128 ? p.rows : 128;
+        }
         return launch_attn_merge_tc(a, d->D, p.items, p.max_splits, st);
     }
     if (d->D == 128) return launch_attn<128>(a, mask, p, d->Hkv, n_out, st);
@@ -891,4 +907,25 @@ extern "C" int specroll_tree_attn_paged(const specroll_attn_desc *d, const void 
     if (!lengths_to_indptr(kv_len_host, d->B, &ip)) return SPECROLL_EINVAL;
     return run_tree_attn(d, Q, Kp, Vp, n_pages * SPECROLL_PAGE_TOKENS, nullptr, kv_len_dev, page_indptr_dev,
                          page_table_dev, ip.data(), Kt, Vt, parent_host, O, lse, workspace, workspace_bytes, cuda_stream);
+}
+
+extern "C" size_t specroll_tree_attn_kv4_workspace_bytes(const specroll_attn_desc *d, const int32_t *kv_len_host) {
+    if (!d || !kv_len_host || d->B < 0 || d->B > (1 << 24)) return 0;
+    std::vector<int32_t> ip;
+    if (!lengths_to_indptr(kv_len_host, d->B, &ip)) return 0;
+    AttnPlan p;
+    if (make_attn_plan(d, ip.data(), &p, true) != SPECROLL_OK || !p.use_tc) return 0;
+    return p.total;
+}
+
+extern "C" int specroll_tree_attn_kv4(const specroll_attn_desc *d, const void *Q, const void *pool, int64_t n_pages,
+                                      const int32_t *page_table_dev, const int32_t *page_indptr_dev, const int32_t *kv_len_dev,
+                                      const int32_t *kv_len_host, const void *Kt, const void *Vt, const int32_t *parent_host, void *O,
+                                      float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!d || !kv_len_host || d->B < 0 || d->B > (1 << 24) || n_pages < 0 || n_pages > (1LL << 24) || !page_table_dev)
+        return SPECROLL_EINVAL;
+    std::vector<int32_t> ip;
+    if (!lengths_to_indptr(kv_len_host, d->B, &ip)) return SPECROLL_EINVAL;
+    return run_tree_attn(d, Q, nullptr, nullptr, n_pages * SPECROLL_PAGE_TOKENS, nullptr, kv_len_dev, page_indptr_dev, page_table_dev, ip.data(),
+                         Kt, Vt, parent_host, O, lse, workspace, workspace_bytes, cuda_stream, true, pool);
 }

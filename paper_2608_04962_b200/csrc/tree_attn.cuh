@@ -30,6 +30,9 @@ struct AttnArgs {
     int early_cache;              // plan, cache and page table were complete before the preceding kernel was launched
     float *hand;                  // [ATTN_HAND_CTAS][4][128] per-CTA hand-over area between two groups of warps of the tcgen05 kernel
     int32_t merge_mode;           // chunks of a split sequence are merged 0: by the CTA that finishes last; 2: by a later kernel
+    // 4-bit paged cache only
+    const uint8_t *pool;          // u8 [n_pages][Hkv][2][tile]
+    int32_t n_pages;
     int32_t no_pdl;               // launch the attention kernel as an ordinary kernel, not as a programmatic dependent
 };
 
@@ -37,6 +40,8 @@ constexpr int ATTN_HAND_CTAS = 256;  // CTAs the hand-over area is sized for (th
 
 // tcgen05 kernel (tree_attn_tc.cu).  T_kv = total cached tokens.  Launches the main kernel only.
 int launch_attn_tc(const AttnArgs &a, const TopoMask &mask, int D, long long T_kv, int32_t *status, cudaStream_t st);
+// Kernel for a 4-bit cache and few query rows per KV head (tree_attn_kv4.cu); the same plan and partials.
+int launch_attn_kv4(const AttnArgs &a, const TopoMask &mask, int D, int32_t *status, cudaStream_t st);
 // Merges the chunks of split sequences after launch_attn_tc when a.merge_mode == 2.  items = chunks in the plan, max_splits = those of
 // the longest sequence.
 int launch_attn_merge_tc(const AttnArgs &a, int D, int items, int max_splits, cudaStream_t st);
