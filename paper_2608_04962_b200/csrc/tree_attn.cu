@@ -512,6 +512,7 @@ __global__ void __launch_bounds__(128) attn_combine_kernel(AttnArgs a) {
 // ------------------------------------------------------------------------------ host side
 
 constexpr int PLAN_SMS = 148;  // SMs the chunking is planned for
+constexpr int KV4_FEW_ROWS = 16;  // 4-bit cache: query rows per KV head up to which the mma.sync kernel takes the call
 
 // Chunks of the sequences (tile counts) when none may hold more than ct tiles, and the most a sequence has.
 static long long count_chunks(const std::vector<int> &tiles, int ct, int *max_ns) {
@@ -570,7 +571,7 @@ struct AttnPlan {
     int max_splits;  // chunks of the longest sequence
     int merge_mode;  // tcgen05 path: 0 = split sequences are merged inside the attention kernel, 2 = by a kernel after it
     bool use_tc;
-    bool kv4;        // 4-bit cache
+    bool kv4_few;    // 4-bit cache, few query rows: tree_attn_kv4.cu
     size_t off_status, off_items, off_sorted, off_rank, off_tab, off_counters, off_po, off_pml, off_hand, total;
 };
 
@@ -585,10 +586,10 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     p->tile_tokens = p->use_tc ? 128 : AT_BN;  // KV tokens per tile of the chosen kernel
     const int TT = p->tile_tokens;
     p->rows = d->N * G;
-    p->kv4 = kv4;
+    p->kv4_few = p->use_tc && kv4 && p->rows <= KV4_FEW_ROWS;
     int places = PLAN_SMS;  // CTAs that run side by side
-    if (kv4) {
-        // 8 or 16 rows a CTA, which need not be whole nodes
+    if (p->kv4_few) {
+        // 8 or 16 rows a CTA
         p->rows_per_block = p->rows <= 8 ? 8 : 16;
         p->n_rb = (p->rows + p->rows_per_block - 1) / p->rows_per_block;
         p->nodes_per_block = 0;
@@ -674,7 +675,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     if (max_tiles / p->chunk_tiles + 1 > 65535) return SPECROLL_EINVAL;
     p->max_splits = (max_tiles + p->chunk_tiles - 1) / p->chunk_tiles;
     p->merge_mode = (p->use_tc && merge_by_kernel((long long)items * ctas_per_tile, (max_tiles + p->chunk_tiles - 1) / p->chunk_tiles)) ? 2 : 0;
-    if (kv4) p->merge_mode = 2;  // (its CTAs leave when their chunk is done)
+    if (p->kv4_few) p->merge_mode = 2;  // (its CTAs leave when their chunk is done)
     if (p->use_tc && items == d->B) p->merge_mode = 2;  // (nothing is split: nothing is merged anywhere)
     p->n_counters = 64 + d->B * d->Hkv * p->n_rb;  // [0]: work counter, [1]: CTAs that have left; [64 ...]: per (b, hkv, rb) arrivals
     size_t o = 0;
@@ -834,6 +835,7 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     a.total_work = p.items * d->Hkv * p.n_rb;
     a.merge_mode = p.merge_mode;
     a.nodes_per_block = p.nodes_per_block;
+    a.kv4 = kv4 ? 1 : 0;
     a.pool = static_cast<const uint8_t *>(pool4);
     a.n_pages = kv4 ? (int32_t)(T_kv / SPECROLL_PAGE_TOKENS) : 0;
     a.no_pdl = (d->flags & SPECROLL_ATTN_NO_PDL) ? 1 : 0;
@@ -850,9 +852,9 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     }
     const size_t n_out = (size_t)d->B * d->N * d->Hq;
     if (p.use_tc) {
-        const int rc = p.kv4 ? launch_attn_kv4(a, mask, d->D, status, st) : launch_attn_tc(a, mask, d->D, T_kv, status, st);
+        const int rc = p.kv4_few ? launch_attn_kv4(a, mask, d->D, status, st) : launch_attn_tc(a, mask, d->D, T_kv, status, st);
         if (rc != SPECROLL_OK || p.merge_mode != 2 || p.items <= d->B) return rc;
-        if (p.kv4) {  // (the merge takes up to 128 rows a block, whatever the attention's blocks were)
+        if (p.kv4_few) {  // (the merge takes up to 128 rows a block, whatever the attention's blocks were)
             a.n_rb = (p.rows + 127) / 128;
             a.rows_per_block = p.rows < 128 ? p.rows : 128;
         }

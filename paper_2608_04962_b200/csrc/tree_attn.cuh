@@ -31,6 +31,7 @@ struct AttnArgs {
     float *hand;                  // [ATTN_HAND_CTAS][4][128] per-CTA hand-over area between two groups of warps of the tcgen05 kernel
     int32_t merge_mode;           // chunks of a split sequence are merged 0: by the CTA that finishes last; 2: by a later kernel
     // 4-bit paged cache only
+    int32_t kv4;                  // the cache is one
     const uint8_t *pool;          // u8 [n_pages][Hkv][2][tile]
     int32_t n_pages;
     int32_t no_pdl;               // launch the attention kernel as an ordinary kernel, not as a programmatic dependent

@@ -42,6 +42,7 @@
 // kernel) the loading thread fetches its first cache tiles before the wait that precedes every other access.
 #include <math.h>
 
+#include "kv4.cuh"
 #include "tc05.cuh"
 #include "tree_attn.cuh"
 
@@ -57,18 +58,23 @@ struct UnitDesc {
     int32_t valid, b, hkv, rb, n_splits, kv0, L, t_lo, n_it, has_tree, item, item0;
 };
 
-template <int D, bool TEAMS>
+template <int D, bool TEAMS, bool KV4>
 struct Cfg {
     static constexpr int NBOX = D / 64;
     static constexpr int SB = 3;   // S buffers
     // K and V tiles share ONE ring, filled in the order they are consumed (K0 K1 K2 V0 K3 V1 K4 V2 ...: S runs
     // three tiles ahead of P V), so every load has the whole ring's depth to land; separate rings would need
     // three stages each for that, which does not fit beside two Q buffers.
-    static constexpr int RS = 5;   // ring stages
+    static constexpr int RS = KV4 ? 4 : 5;   // ring stages
+    // 4-bit cache: K and V of a page arrive as codes in SS staging slots; four warps decode them into the ring's stages
+    static constexpr int SS = KV4 ? 3 : 0, SLOT_BYTES = KV4 ? Kv4<D>::TILE : 0, DECODE_WARPS = KV4 ? 4 : 0;
     static constexpr int QS = 2;   // Q buffers (units)
     static constexpr int MMA_WARPS = 2;  // issuing threads (one lane of each)
     static constexpr int SOFTMAX_THREADS = 256, OUT_THREADS = 128;
-    static constexpr int THREADS = 32 * (1 + MMA_WARPS) + SOFTMAX_THREADS + OUT_THREADS;
+    // first warps of the softmax, output and decoding roles (whole groups of four where there is decoding)
+    static constexpr int SOFT0 = KV4 ? 4 : 1 + MMA_WARPS, OUT0 = SOFT0 + SOFTMAX_THREADS / 32, DECODE0 = OUT0 + OUT_THREADS / 32;
+    static constexpr int THREADS = 32 * (DECODE0 + DECODE_WARPS);
+    static constexpr int FULL_ARRIVALS = KV4 ? DECODE_WARPS : 1;  // of a ring stage: the decoding warps, or the loading thread
     static constexpr int Q_BYTES = NBOX * BOX_BYTES;   // the Q block of one unit
     static constexpr int KV_BYTES = NBOX * BOX_BYTES;  // one K tile or one V tile
     // barrier slots
@@ -76,18 +82,18 @@ struct Cfg {
                          B_PVDONE = B_PREADY + SB, B_QFULL = B_PVDONE + SB, B_QFREE = B_QFULL + QS,
                          B_UFULL = B_QFREE + QS, B_UEMPTY = B_UFULL + 2, B_X = B_UEMPTY + 2, B_ALL = B_X + 4,
                          B_OFULL = B_ALL + 1, B_OFREE = B_OFULL + 1, B_HFULL = B_OFREE + 1, B_HFREE = B_HFULL + 1,
-                         N_BARS = B_HFREE + 1;
+                         B_SFILLED = B_HFREE + 1, B_SFREE = B_SFILLED + SS, N_BARS = B_SFREE + SS;
     static constexpr int BAR_BYTES = (8 * N_BARS + 15) / 16 * 16;
     // exchange area: the rows' reference maxima as one softmax team leaves them for the other ([2][128] fp32), or
     // the partial row maxima of the pairs (per lane group [2 slots][2 halves][32 lanes] bf16)
     static constexpr int XCH_BYTES = 1024;
-    static constexpr int EXTRA = BAR_BYTES + 16 + XCH_BYTES + 2 * 64;  // barriers, slot/abort/ticket, exchange, ring
+    static constexpr int EXTRA = BAR_BYTES + 16 + XCH_BYTES + 2 * 64 + 16 * SS;  // barriers, slot/abort/ticket, exchange, ring, slots' jobs
     // hand-over from the softmax warps to the output warps (per row: each team's share of the sum and the
     // reference maximum it is relative to): in global memory, one area per CTA, because shared memory is full
     static constexpr int HAND_FLOATS = 4 * 128;
     // The operand tiles need 1024-byte alignment.  The dynamic shared window starts 1024-aligned on this
     // architecture (checked at run time: the kernel reports an error instead of running misaligned).
-    static constexpr int USED = QS * Q_BYTES + RS * KV_BYTES + EXTRA;
+    static constexpr int USED = QS * Q_BYTES + RS * KV_BYTES + SS * SLOT_BYTES + EXTRA;
     // at least ~118 KB so that two CTAs can never share an SM (each allocates all of TMEM)
     static constexpr int SMEM = USED > 120832 ? USED : 120832;
     static constexpr uint32_t O_COL = 0, S_COL = 128;
@@ -135,14 +141,19 @@ __device__ __forceinline__ float bf16_bits_to_float(unsigned short b) { return _
 // ONE: every CTA has one unit at most (few sequences): the second Q buffer is free for the hand-over area, and nothing is
 // counted - the merge, if any, is a kernel of its own - so the CTA leaves without a round trip to memory.  (A template flag:
 // asked at run time it cost the shapes with many units 1-4 %.)
-template <int D, bool TEAMS, bool ONE>
-__global__ void __launch_bounds__(attc::Cfg<D, TEAMS>::THREADS, 1)
+// KV4: the cache is a 4-bit paged pool (tmK and tmV are not used).  Pages come as codes into staging slots by untiled bulk copies; four
+// warps more take the slots in order and decode them into the ring's stages, in the 128-byte swizzle that TMA would have left.  The
+// tree's tiles go through the same queue, as a slot that names the tile, and are fetched into their stages from there: the ring's
+// stages are filled by the decoding warps alone, in one order, so that a stage's barrier is never a phase further behind than its parity
+// can tell.
+template <int D, bool TEAMS, bool ONE, bool KV4>
+__global__ void __launch_bounds__(attc::Cfg<D, TEAMS, KV4>::THREADS, 1)
 tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKt,
                     const __grid_constant__ CUtensorMap tmVt, AttnArgs a, TopoMask mask,
                     int32_t *__restrict__ status) {
     using namespace attc;
-    using C = Cfg<D, TEAMS>;
+    using C = Cfg<D, TEAMS, KV4>;
     constexpr int DH = D / 2;  // accumulator columns per thread of a pair (rescaling)
     constexpr int SB = C::SB, RS = C::RS, QS = C::QS, THREADS = C::THREADS;
     extern __shared__ unsigned char smem_raw[];
@@ -151,14 +162,18 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     unsigned char *aligned = smem_raw + (base - raw);
     const uint32_t q_s = base;
     const uint32_t r_s = base + QS * C::Q_BYTES;  // the K/V ring
-    const uint32_t bar0 = r_s + RS * C::KV_BYTES;
+    const uint32_t g_s = r_s + RS * C::KV_BYTES;  // the staging slots
+    const uint32_t bar0 = g_s + C::SS * C::SLOT_BYTES;
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
-    unsigned char *extra = aligned + QS * C::Q_BYTES + RS * C::KV_BYTES + C::BAR_BYTES;
+    unsigned char *extra = aligned + QS * C::Q_BYTES + RS * C::KV_BYTES + C::SS * C::SLOT_BYTES + C::BAR_BYTES;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(extra);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(extra + 4);
     volatile int *tickets = reinterpret_cast<volatile int *>(extra + 8);
     unsigned char *xch_base = extra + 16;
     volatile UnitDesc *ring = reinterpret_cast<volatile UnitDesc *>(extra + 16 + C::XCH_BYTES);  // 2 slots of 64 bytes
+    // 4-bit cache: per staging slot, the ring position it goes to (-1: no more), what it is, and of a tree's tile its KV head and first row
+    enum Job { NO_PAGE, CODES, TREE_K, TREE_V };
+    volatile int *const slot_job = reinterpret_cast<volatile int *>(extra + 16 + C::XCH_BYTES + 2 * 64);
     constexpr bool one_wave = ONE;
     // [l of team 0 | l of team 1 | m of team 0 | m of team 1][128 rows]
     float *hand = a.hand + (size_t)blockIdx.x * C::HAND_FLOATS;
@@ -169,13 +184,15 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     auto twait = [&](int, uint32_t b_, uint32_t par_) { return mbar_wait(b_, par_, abort_flag); };
     // Ring stage and phase of tile t's K and V (t counts tiles over all units of this CTA): in load order
     // K0 K1 K2 V0 K3 V1 K4 V2 ... K(t) is load number 2t - 2 (t for the first two) and V(t) load number 2t + 3.
+    auto k_pos = [](uint32_t t) -> uint32_t { return t < 2u ? t : 2u * t - 2u; };
+    auto v_pos = [](uint32_t t) -> uint32_t { return 2u * t + 3u; };
     auto k_slot = [&](uint32_t t, int &st, uint32_t &ph) {
-        const uint32_t pos = t < 2u ? t : 2u * t - 2u;
+        const uint32_t pos = k_pos(t);
         st = (int)(pos % RS);
         ph = (pos / RS) & 1u;
     };
     auto v_slot = [&](uint32_t t, int &st, uint32_t &ph) {
-        const uint32_t pos = 2u * t + 3u;
+        const uint32_t pos = v_pos(t);
         st = (int)(pos % RS);
         ph = (pos / RS) & 1u;
     };
@@ -188,6 +205,8 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::N_BARS; ++i) {
             uint32_t count = 1;
+            if (i >= C::B_FULL && i < C::B_FULL + RS) count = C::FULL_ARRIVALS;
+            if (KV4 && i >= C::B_SFREE && i < C::B_SFREE + C::SS) count = C::DECODE_WARPS;
             // a tile's P comes from one team, or from all softmax threads
             if (i >= C::B_PREADY && i < C::B_PREADY + SB) count = TEAMS ? C::SOFTMAX_THREADS / 2 : C::SOFTMAX_THREADS;
             // a unit's descriptor is read by the MMA threads, the softmax threads and the output threads
@@ -295,7 +314,32 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const CUtensorMap *pv_map[2];
             int pv_h[2], pv_tok[2];
             int n_pend = 0;
+            // 4-bit cache: the job for ring position pos (codes of a page: K where kind is TREE_K, else V; or the tree's tile) into the next slot
+            uint32_t staged = 0;
+            auto slot_free = [&]() { return bar(C::B_SFREE + (int)(staged % (C::SS ? C::SS : 1))); };
+            auto slot_parity = [&]() { return ((staged / (C::SS ? C::SS : 1)) & 1u) ^ 1u; };
+            auto post = [&](bool tree, int kind, int hkv, int at, uint32_t pos) -> bool {
+                if constexpr (KV4) {
+                    const int s = (int)(staged % C::SS);
+                    if (!twait(5, slot_free(), slot_parity())) return false;
+                    ++staged;
+                    const bool codes = !tree && at >= 0 && at < a.n_pages;
+                    slot_job[4 * s] = (int)pos;
+                    slot_job[4 * s + 1] = tree ? kind : codes ? CODES : NO_PAGE;
+                    slot_job[4 * s + 2] = hkv;
+                    slot_job[4 * s + 3] = at;
+                    if (codes) {
+                        mbar_arrive_expect_tx(bar(C::B_SFILLED + s), C::SLOT_BYTES);
+                        bulk_load(g_s + s * C::SLOT_BYTES, a.pool + (((size_t)at * a.Hkv + hkv) * 2 + (kind == TREE_V)) * C::SLOT_BYTES,
+                                  C::SLOT_BYTES, bar(C::B_SFILLED + s));
+                    } else {
+                        mbar_arrive(bar(C::B_SFILLED + s));
+                    }
+                }
+                return true;
+            };
             auto load_v = [&](const CUtensorMap *mv, int hkv, int tok) -> bool {
+                if (KV4) return post(mv == &tmVt, TREE_V, hkv, tok, v_pos(vt++));  // (tok: the page, or the tree's first row)
                 int s;
                 uint32_t ph;
                 v_slot(vt, s, ph);
@@ -381,24 +425,32 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 int pg0 = (pt && n_kv > 0) ? __ldg(pt) : 0, pg1 = (pt && n_kv > 1) ? __ldg(pt + 1) : 0;
                 for (int it = 0; it < n_it && ok; ++it) {
                     const int pg2 = (pt && it + 2 < n_kv) ? __ldg(pt + it + 2) : 0;
-                    int s;
-                    uint32_t kph;
-                    k_slot(kt, s, kph);
-                    if (!twait(3, bar(C::B_EMPTY + s), kph ^ 1u)) {
-                        ok = false;
-                        break;
-                    }
                     const bool tree = has_tree && (it == n_it - 1);
-                    if (q_pending && (tree || it >= 3)) settle();
-                    const int tok = tree ? b * N : (pt ? pg0 * BN : kv0 + (t_lo + it) * BN);
+                    const int tok = tree ? b * N : (KV4 ? pg0 : pt ? pg0 * BN : kv0 + (t_lo + it) * BN);
                     pg0 = pg1;
                     pg1 = pg2;
-                    const CUtensorMap *mk = tree ? &tmKt : &tmK;
-                    const uint32_t dst = stage_addr(s);
-                    mbar_arrive_expect_tx(bar(C::B_FULL + s), C::KV_BYTES);
+                    if constexpr (KV4) {
+                        if (q_pending && (tree || it >= 3)) settle();
+                        if (!post(tree, TREE_K, hkv, tok, k_pos(kt))) {
+                            ok = false;
+                            break;
+                        }
+                    } else {
+                        int s;
+                        uint32_t kph;
+                        k_slot(kt, s, kph);
+                        if (!twait(3, bar(C::B_EMPTY + s), kph ^ 1u)) {
+                            ok = false;
+                            break;
+                        }
+                        if (q_pending && (tree || it >= 3)) settle();
+                        const CUtensorMap *mk = tree ? &tmKt : &tmK;
+                        const uint32_t dst = stage_addr(s);
+                        mbar_arrive_expect_tx(bar(C::B_FULL + s), C::KV_BYTES);
 #pragma unroll
-                    for (int bx = 0; bx < C::NBOX; ++bx)
-                        tma_load_3d(dst + bx * BOX_BYTES, mk, bx * 64, hkv, tok, bar(C::B_FULL + s));
+                        for (int bx = 0; bx < C::NBOX; ++bx)
+                            tma_load_3d(dst + bx * BOX_BYTES, mk, bx * 64, hkv, tok, bar(C::B_FULL + s));
+                    }
                     ++kt;
                     if (n_pend == 2) {
                         ok = load_v(pv_map[0], pv_h[0], pv_tok[0]);
@@ -419,6 +471,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     int s;
                     uint32_t ph;
                     v_slot(vt, s, ph);
+                    if (KV4) return mbar_test_wait(slot_free(), slot_parity());
                     return mbar_test_wait(bar(C::B_EMPTY + s), ph ^ 1u);
                 };
                 while (ok && n_pend > 0 && v_stage_free()) {
@@ -434,6 +487,13 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             asm volatile("griddepcontrol.wait;" ::: "memory");
             // flush the V tiles still pending (the last two tiles of the last unit)
             for (int i = 0; i < n_pend && ok; ++i) ok = load_v(pv_map[i], pv_h[i], pv_tok[i]);
+            if constexpr (KV4) {
+                const int s = (int)(staged % C::SS);
+                if (ok && (ok = twait(6, slot_free(), slot_parity()))) {
+                    slot_job[4 * s] = -1;
+                    mbar_arrive(bar(C::B_SFILLED + s));
+                }
+            }
             if (!ok) {
                 // aborting: give copies in flight time to land before the CTA goes away
                 const unsigned long long t0 = globaltimer_ns();
@@ -534,13 +594,80 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 }
             }
         }
-    } else if (warp >= 1 + C::MMA_WARPS + C::SOFTMAX_THREADS / 32) {
+    } else if (warp < C::SOFT0) {
+        // (fills the group of four)
+    } else if (KV4 && warp >= C::DECODE0) {
+        // ------------------------------------------------------------------ codes to bf16 (4 warps)
+        // A warp has 8 (D = 128) or 16 tokens at a time, a thread one block of 32 elements: 16 bytes of codes, one scale, four 16-byte
+        // chunks of the stage.  Threads of a token's second box take their chunks in another order, so that eight neighbouring threads
+        // write eight different bank groups.
+        if constexpr (KV4) {
+            constexpr int PER = D / 32, STEP = 32 / PER;  // threads of a token, tokens of a warp's step
+            const int dw = warp - C::DECODE0, c = lane % PER, flip = D == 128 ? (c >> 1) * 2 : 0;
+            bool ok = true;
+            for (uint32_t n = 0; ok; ++n) {
+                const int s = (int)(n % C::SS);
+                ok = twait(0, bar(C::B_SFILLED + s), (n / C::SS) & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const int pos = slot_job[4 * s], kind = slot_job[4 * s + 1];
+                if (pos < 0) break;
+                const int st = pos % RS;
+                ok = twait(1, bar(C::B_EMPTY + st), (((uint32_t)pos / RS) & 1u) ^ 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (kind >= TREE_K) {
+                    if (lane == 0) {
+                        if (dw == 0) {
+                            const CUtensorMap *map = kind == TREE_K ? &tmKt : &tmVt;
+                            mbar_arrive_expect_tx(bar(C::B_FULL + st), C::KV_BYTES);
+#pragma unroll
+                            for (int bx = 0; bx < C::NBOX; ++bx)
+                                tma_load_3d(stage_addr(st) + bx * BOX_BYTES, map, bx * 64, slot_job[4 * s + 2], slot_job[4 * s + 3],
+                                            bar(C::B_FULL + st));
+                        } else {
+                            mbar_arrive(bar(C::B_FULL + st));
+                        }
+                        mbar_arrive(bar(C::B_SFREE + s));
+                    }
+                    __syncwarp();
+                    continue;
+                }
+                const unsigned char *codes = aligned + QS * C::Q_BYTES + RS * C::KV_BYTES + s * C::SLOT_BYTES;
+                const uint32_t dst = stage_addr(st) + (D == 128 ? (uint32_t)(c >> 1) * BOX_BYTES : 0u);
+                const uint32_t keep = kind == CODES ? 0xffffffffu : 0u;  // (no such page: zeros)
+#pragma unroll
+                for (int it = 0; it < BN / (4 * STEP); ++it) {
+                    const int tok = (it * 4 + dw) * STEP + lane / PER;
+                    const uint4 w = *reinterpret_cast<const uint4 *>(codes + tok * Kv4<D>::ROW + 16 * c);
+                    const uint32_t sb = codes[Kv4<D>::CODES + tok * Kv4<D>::SROW + c];
+                    const uint32_t s2 = kv4_scale_pair(sb, sb) & keep, o2 = kv4_offset(s2);
+                    const uint32_t ww[4] = {flip ? w.z : w.x, flip ? w.w : w.y, flip ? w.x : w.z, flip ? w.y : w.w};
+                    const uint32_t row = dst + (uint32_t)tok * 128u;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t r[4];
+                        kv4_word(ww[i], s2, o2, r);
+                        const uint32_t chunk = (uint32_t)((c & 1) * 4 + (i ^ flip)) ^ (uint32_t)(tok & 7);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + chunk * 16u), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+                                     : "memory");
+                    }
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(C::B_FULL + st));
+                    mbar_arrive(bar(C::B_SFREE + s));
+                }
+            }
+        }
+    } else if (warp >= C::OUT0) {
         // ------------------------------------------------------------------ output (4 warps, one thread per query row)
         // Takes a finished unit's accumulator out of TMEM while the other warps are already in the next unit.
         const int lg = warp & 3;  // TMEM lane group of this warp
         const int row = lg * 32 + lane;
         const uint32_t t_lane = tmem_base + ((uint32_t)(lg * 32) << 16);
-        const int tix = (int)threadIdx.x - (32 * (1 + C::MMA_WARPS) + C::SOFTMAX_THREADS);
+        const int tix = (int)threadIdx.x - 32 * C::OUT0;
         const uint32_t all_bar = bar(C::B_ALL);
         uint32_t use_all = 0;
         bool ok = true;
@@ -657,7 +784,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             // left after the tile before: if that reference differs from its own, or the alarm went off (both
             // rare), the tile is done again from S with the two passes of a first tile, which can move the
             // reference and rescale the accumulator.  The result is the same as doing two passes every time.
-            const int ws = warp - (1 + C::MMA_WARPS);
+            const int ws = warp - C::SOFT0;
             const int team = ws >> 2;
             const int lg = warp & 3;  // TMEM lane group of this warp
             const int row = lg * 32 + lane;
@@ -869,7 +996,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             }
         } else {
             // ------------------------------------------------------------------ softmax (8 warps, two threads per query row)
-            const int ws = warp - (1 + C::MMA_WARPS);
+            const int ws = warp - C::SOFT0;
             const int half = ws >> 2;  // which 64 of a tile's 128 columns, and which D/2 accumulator columns
             const int lg = warp & 3;   // TMEM lane group of this warp
             const int row = lg * 32 + lane;
@@ -1116,16 +1243,17 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
 }
 
-template <int D, bool TEAMS>
+template <int D, bool TEAMS, bool KV4>
 static int launch_tc(const AttnArgs &a, const TopoMask &mask, long long T_kv, int32_t *status, cudaStream_t st) {
-    using C = attc::Cfg<D, TEAMS>;
+    using C = attc::Cfg<D, TEAMS, KV4>;
     CUtensorMap tmQ, tmK, tmV, tmKt, tmVt;
     int rc;
     const uint64_t tree_rows = (uint64_t)a.B * a.N;
     // an empty cache still needs well-formed maps; they are never used for a load then
-    const void *kc = T_kv > 0 ? (const void *)a.Kc : (const void *)a.Kt;
-    const void *vc = T_kv > 0 ? (const void *)a.Vc : (const void *)a.Vt;
-    const uint64_t cache_rows = T_kv > 0 ? (uint64_t)T_kv : tree_rows;
+    const bool cached = T_kv > 0 && !KV4;
+    const void *kc = cached ? (const void *)a.Kc : (const void *)a.Kt;
+    const void *vc = cached ? (const void *)a.Vc : (const void *)a.Vt;
+    const uint64_t cache_rows = cached ? (uint64_t)T_kv : tree_rows;
     if ((rc = make_tmap_3d_bf16(&tmQ, a.Q, D, a.Hq, tree_rows, (uint32_t)a.G, (uint32_t)a.nodes_per_block)) != SPECROLL_OK)
         return rc;
     if ((rc = make_tmap_3d_bf16(&tmK, kc, D, a.Hkv, cache_rows, 1, attc::BN)) != SPECROLL_OK) return rc;
@@ -1136,7 +1264,7 @@ static int launch_tc(const AttnArgs &a, const TopoMask &mask, long long T_kv, in
     if ((rc = device_setup(nullptr, 0, &n_sm)) != SPECROLL_OK) return rc;
     const int ctas = n_sm < ATTN_HAND_CTAS ? n_sm : ATTN_HAND_CTAS;  // every CTA has a hand-over area of its own
     const unsigned grid = (unsigned)(a.total_work < ctas ? a.total_work : ctas);
-    auto *const kern = a.total_work <= (int)grid && a.merge_mode != 0 ? tree_attn_tc_kernel<D, TEAMS, true> : tree_attn_tc_kernel<D, TEAMS, false>;
+    auto *const kern = a.total_work <= (int)grid && a.merge_mode != 0 ? tree_attn_tc_kernel<D, TEAMS, true, KV4> : tree_attn_tc_kernel<D, TEAMS, false, KV4>;
     if ((rc = device_setup(reinterpret_cast<const void *>(kern), C::SMEM, nullptr)) != SPECROLL_OK) return rc;
     // Programmatic stream serialization: the CTAs may be set up (barriers, tensor memory, zeroed Q buffers) while
     // the kernel before this one in the stream is still running its last CTAs; the kernel itself waits for
@@ -1270,8 +1398,9 @@ int launch_attn_tc(const AttnArgs &a, const TopoMask &mask, int D, long long T_k
     // One row block per (sequence, KV head): the kernel is bound by HBM and the softmax with two threads per row
     // is (slightly) the better one; more blocks: bound by the softmax, where the two alternating teams are faster.
     const bool teams = a.n_rb > 1;
-    if (D == 128) return teams ? launch_tc<128, true>(a, mask, T_kv, status, st) : launch_tc<128, false>(a, mask, T_kv, status, st);
-    return teams ? launch_tc<64, true>(a, mask, T_kv, status, st) : launch_tc<64, false>(a, mask, T_kv, status, st);
+    if (a.kv4) return D == 128 ? launch_tc<128, true, true>(a, mask, T_kv, status, st) : launch_tc<64, true, true>(a, mask, T_kv, status, st);
+    if (D == 128) return teams ? launch_tc<128, true, false>(a, mask, T_kv, status, st) : launch_tc<128, false, false>(a, mask, T_kv, status, st);
+    return teams ? launch_tc<64, true, false>(a, mask, T_kv, status, st) : launch_tc<64, false, false>(a, mask, T_kv, status, st);
 }
 
 }  // namespace specroll
