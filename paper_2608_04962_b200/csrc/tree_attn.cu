@@ -186,39 +186,53 @@ attn_prep_kernel(const int32_t *__restrict__ kv_indptr, const int32_t *__restric
     if (t == 0) item_start[B] = total;
     if (!sorted_start) return;
     __syncthreads();
-    // rank by counting: position of b in the order (cost descending, index ascending)
-    for (int b = t; b < B; b += PREP_THREADS) {
-        const int c = sh_cost[b];
-        int r = 0;
-        for (int o = 0; o < B; ++o) {
-            const int co = sh_cost[o];
-            r += (co > c) || (co == c && o < b);
+    // rank by counting: position of b in the order (cost descending, index ascending); where there are fewer sequences than threads
+    // several threads count for one.  The ranks take the costs' place, the chunk counts in work order that of the prefix.
+    {
+        int per = 1;
+        while (per < 32 && 2 * per * B <= PREP_THREADS) per *= 2;
+        int rank[PREP_MAX_B / PREP_THREADS];
+#pragma unroll
+        for (int q = 0; q < PREP_MAX_B / PREP_THREADS; ++q) {
+            const int i = q * PREP_THREADS + t, b = i / per;
+            int r = 0;
+            if (b < B) {
+                const int c = sh_cost[b];
+                for (int o = i % per; o < B; o += per) {
+                    const int co = sh_cost[o];
+                    r += (co > c) || (co == c && o < b);
+                }
+            }
+            for (int o = 1; o < per; o *= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
+            rank[q] = r;
         }
-        seq_at_rank[r] = b;
-        sh_tmp[r] = (int)sh_ns[b];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < PREP_MAX_B / PREP_THREADS; ++q) {
+            const int i = q * PREP_THREADS + t, b = i / per;
+            if (b >= B || i % per) continue;
+            seq_at_rank[rank[q]] = b;
+            sh_cost[b] = rank[q];
+            sh_tmp[rank[q]] = (int)sh_ns[b];
+        }
     }
     __syncthreads();
     const int total2 = block_exclusive_scan(sh_tmp, B, warp_tot);
     for (int r = t; r < B; r += PREP_THREADS) sorted_start[r] = sh_tmp[r];
     if (t == 0) sorted_start[B] = total2;
-    // per-chunk table in work order, so that the scheduler decodes a work unit with one 32-byte load
+    // per-chunk table in work order, so that the scheduler decodes a work unit with one 32-byte load; again several threads a sequence
     if (unit_tab) {
         __syncthreads();
-        for (int b = t; b < B; b += PREP_THREADS) {
-            // recompute this sequence's rank (same rule as above) to find where its chunks go
-            const int c = sh_cost[b];
-            int r = 0;
-            for (int o = 0; o < B; ++o) {
-                const int co = sh_cost[o];
-                r += (co > c) || (co == c && o < b);
-            }
-            const int ns = (int)sh_ns[b];
+        int per = 1;
+        while (per < 32 && 2 * per * B <= PREP_THREADS) per *= 2;
+        for (int i = t; i < B * per; i += PREP_THREADS) {
+            const int b = i / per, ns = (int)sh_ns[b];
             // contiguous cache: first token and length; paged cache: first slot of the page table and length
             const int kv0 = kv_len ? page_indptr[b] : kv_indptr[b];
             const int L = kv_len ? kv_len[b] : kv_indptr[b + 1] - kv0;
             const int first = item_start[b];  // written by this block; visible after the barriers above
-            int4 *dst = reinterpret_cast<int4 *>(unit_tab) + 2 * (size_t)sh_tmp[r];
-            for (int s = 0; s < ns; ++s) {
+            int4 *dst = reinterpret_cast<int4 *>(unit_tab) + 2 * (size_t)sh_tmp[sh_cost[b]];
+            for (int s = i % per; s < ns; s += per) {
                 dst[2 * s] = make_int4(b, s, ns, first);
                 dst[2 * s + 1] = make_int4(kv0, L, 0, 0);
             }
@@ -593,7 +607,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
         p->rows_per_block = p->rows <= 8 ? 8 : 16;
         p->n_rb = (p->rows + p->rows_per_block - 1) / p->rows_per_block;
         p->nodes_per_block = 0;
-        if (p->rows_per_block == 8) places = 2 * PLAN_SMS;
+        places = (p->rows_per_block == 8 ? 4 : 3) * PLAN_SMS;
     } else if (p->use_tc) {
         // row blocks are whole nodes: (node, head-in-group) rows of a block are one TMA box
         // The softmax of a row block costs the same whether the block is full or not, so the rows go into as
@@ -854,10 +868,7 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     if (p.use_tc) {
         const int rc = p.kv4_few ? launch_attn_kv4(a, mask, d->D, status, st) : launch_attn_tc(a, mask, d->D, T_kv, status, st);
         if (rc != SPECROLL_OK || p.merge_mode != 2 || p.items <= d->B) return rc;
-        if (p.kv4_few) {  // (the merge takes up to 128 rows a block, whatever the attention's blocks were)
-            a.n_rb = (p.rows + 127) / 128;
-            a.rows_per_block = p.rows < 128 ? p.rows : 128;
-        }
+        if (p.kv4_few) return launch_attn_merge_kv4(a, d->D, st);
         return launch_attn_merge_tc(a, d->D, p.items, p.max_splits, st);
     }
     if (d->D == 128) return launch_attn<128>(a, mask, p, d->Hkv, n_out, st);

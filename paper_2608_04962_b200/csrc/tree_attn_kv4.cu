@@ -1,18 +1,18 @@
 // Tree attention over the 4-bit paged cache, for few query rows per KV head: single tokens and small trees.
 //
 // A CTA takes one chunk of a sequence's pages for one KV head and up to 8 R8 query rows (rows = nodes x query heads of the KV head).
-// Whole pages (K and V codes and scales of the head are one run of 136 D bytes) go into a ring with untiled bulk copies, which the first
-// warp issues on the side; each of the eight warps has 16 of a page's tokens and decodes them straight into mma.sync fragments, so that a cached
-// element passes through shared memory once, as four bits, and is decoded once for all rows:
+// Its four warps go through slices of 32 tokens, each for itself: a warp's first thread fetches its slices (K and V codes and scales)
+// with untiled bulk copies into three stages of its own, so that no warp waits for another before the end.  Codes are decoded
+// straight into mma.sync fragments: a cached element passes through shared memory once, as four bits, and is decoded once for all rows:
 //   S^T (16 tokens x 8 rows)  = K (A operand, from codes) x Q^T (B operand, in registers for the whole unit)
 //   O^T (D x 8 rows)         += V^T (A operand, from codes) x P^T (B operand: P transposed by movmatrix)
 // What an index of a fragment stands for is free as long as both operands agree, and is chosen so that a thread's codes are
 // contiguous: for K a thread has 1/4 of a token's elements (one scale block where D = 128), for V 1/8 of four tokens' elements,
 // paired by byte permutes before decoding.  Tokens of a pair change places in every other pair, which halves the bank conflicts
 // of V's reads.
-// Every warp has a softmax of its own (reference maximum per row, moved only when a score exceeds it by 2^8); the eight meet in
-// shared memory at the end.  The tree's bf16 rows are done by the first warps after the cache.
-// What bounds it: 17 KB of a page in 0.4 us at the HBM rate of one SM, against about 450 issue slots a scheduler for decoding it.
+// Every warp has a softmax of its own (reference maximum per row, moved only when a score exceeds it by 2^8); the four meet in
+// shared memory at the end.  The tree's bf16 rows are done by the warps after their slices, sixteen nodes each.
+// What bounds it: 17 KB of a page in 0.4 us at the HBM rate of one SM, against some 600 issue slots a scheduler for decoding it.
 #include <math.h>
 
 #include "kv4.cuh"
@@ -22,14 +22,16 @@
 namespace specroll {
 
 namespace akv4 {
-constexpr int WARPS = 8, THREADS = 32 * WARPS;
-constexpr int STAGES = 6, LAG = 2;  // a stage is loaded anew LAG tiles after its last use began, when every warp is done with it
+constexpr int WARPS = 4, THREADS = 32 * WARPS;
+constexpr int SLICE = 32, PER_PAGE = SPECROLL_PAGE_TOKENS / SLICE;  // tokens a warp fetches and takes at a time
+constexpr int STAGES = 3;
 constexpr float RESCALE_LOG2 = 8.0f;
 
 template <int D, int R8>
 struct Cfg {
-    static constexpr int PAIR = 2 * Kv4<D>::TILE;  // K and V of a page and head
-    static constexpr int RING = STAGES * PAIR;
+    // a slice: K codes, K scales, V codes, V scales
+    static constexpr int CODES = SLICE * Kv4<D>::ROW, SCALES = SLICE * Kv4<D>::SROW, HALF = CODES + SCALES, BYTES = 2 * HALF;
+    static constexpr int RING = WARPS * STAGES * BYTES;
     static constexpr int RUN = D / 4, STEPS = D / 16;  // a thread's elements of a K row; contraction steps of S
     static constexpr int VRUN = D / 8, MB = D / 16;    // a thread's elements of a V row; row blocks of O^T
     static constexpr int ROWS = 8 * R8;
@@ -37,7 +39,9 @@ struct Cfg {
     static constexpr int O_FLOATS = D * ROWS;
     static constexpr int JOIN = WARPS * (O_FLOATS + 2 * ROWS) * 4;
     static constexpr int BODY = (RING > JOIN ? RING : JOIN);
-    static constexpr int SMEM = BODY + 16 * STAGES + 4 * STAGES + 16;
+    static constexpr int SMEM = BODY + 8 * WARPS * STAGES + 16;
+    static constexpr int CTAS = R8 == 1 ? 4 : 3;  // side by side on an SM: what registers and shared memory have room for
+    static_assert(SCALES % 16 == 0 && CTAS * (SMEM + 1024) <= 233472, "bulk copies; shared memory of an SM");
 };
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
@@ -48,26 +52,20 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
 }  // namespace akv4
 
 template <int D, int R8>
-__global__ void __launch_bounds__(akv4::THREADS, R8 == 1 ? 2 : 1)
+__global__ void __launch_bounds__(akv4::THREADS, (akv4::Cfg<D, R8>::CTAS))
 tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TopoMask mask, int32_t *__restrict__ status) {
     using namespace akv4;
     using C = Cfg<D, R8>;
     extern __shared__ __align__(128) unsigned char smem[];
-    const uint32_t ring_s = smem_u32(smem), bars = ring_s + C::BODY;
-    auto full = [&](int s) { return bars + 8u * (uint32_t)s; };
-    auto empty = [&](int s) { return bars + 8u * (uint32_t)(STAGES + s); };
-    volatile int *const gone = reinterpret_cast<volatile int *>(smem + C::BODY + 16 * STAGES);  // [STAGES]: no such page
-    volatile int *const abort_flag = gone + STAGES;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, c = lane & 3;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(empty(s), WARPS);
-        }
-        *abort_flag = 0;
-        fence_mbar_init();
-    }
+    unsigned char *const mine = smem + warp * STAGES * C::BYTES;  // this warp's stages
+    const uint32_t bars = smem_u32(smem) + C::BODY + 8 * STAGES * warp;
+    volatile int *const abort_flag = reinterpret_cast<volatile int *>(smem + C::BODY + 8 * WARPS * STAGES);
+    if (lane == 0)
+        for (int s = 0; s < STAGES; ++s) mbar_init(bars + 8 * s, 1);
+    if (threadIdx.x == 0) *abort_flag = 0;
+    if (lane == 0) fence_mbar_init();
     __syncthreads();
     pdl_wait();
     pdl_launch_dependents();
@@ -85,6 +83,9 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     const int t_lo = min(tiles_b, split * tps), n_t = min(tiles_b, t_lo + tps) - t_lo;
     const bool has_tree = split == n_splits - 1;
     const int N = a.N, G = a.G, row0 = rb * C::ROWS;
+    // this warp's slices: slice i is tokens first + 128 i .. + 32 of the sequence, a quarter of a page
+    const int first = t_lo * SPECROLL_PAGE_TOKENS + warp * SLICE, end = min(L, (t_lo + n_t) * SPECROLL_PAGE_TOKENS);
+    const int n_i = end > first ? (end - first + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS : 0;
 
     float o[R8][C::MB][4];
     float m[R8][2], l[R8][2];
@@ -98,26 +99,32 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             for (int e = 0; e < 4; ++e) o[r][i][e] = 0.f;
     }
 
-    // ---- loads: tile t into stage t mod STAGES, by one thread (false: a wait ran out)
+    // ---- loads: slice i into stage i mod STAGES, by the warp's first thread.  A page that does not exist is not fetched: its bit in
+    // `absent` makes the decoded values zeros.
     const int32_t *const pt = a.page_table + slot0 + t_lo;
-    int next_page = n_t > 0 && threadIdx.x == 0 ? __ldg(pt) : 0;
-    auto load = [&](int t) -> bool {
-        const int s = t % STAGES, page = next_page;
-        next_page = t + 1 < n_t ? __ldg(pt + t + 1) : 0;
-        if (t >= STAGES && !mbar_wait(empty(s), (t / STAGES - 1) & 1u, abort_flag)) return false;
+    uint32_t absent = 0u;
+    auto load = [&](int i, int page) {
+        const int s = i % STAGES;
         const bool there = page >= 0 && page < a.n_pages;
-        gone[s] = !there;
-        if (there) {
-            mbar_arrive_expect_tx(full(s), C::PAIR);
-            bulk_load(ring_s + s * C::PAIR, a.pool + ((size_t)page * a.Hkv + hkv) * C::PAIR, C::PAIR, full(s));
-        } else {
-            mbar_arrive(full(s));  // (read as zeros)
+        absent = there ? absent & ~(1u << s) : absent | (1u << s);
+        if (lane == 0) {
+            if (there) {
+                const uint32_t dst = smem_u32(mine) + s * C::BYTES, bar = bars + 8 * s;
+                const uint8_t *k = a.pool + ((size_t)page * a.Hkv + hkv) * (2 * Kv4<D>::TILE), *v = k + Kv4<D>::TILE;
+                mbar_arrive_expect_tx(bar, C::BYTES);
+                bulk_load(dst, k + warp * C::CODES, C::CODES, bar);
+                bulk_load(dst + C::CODES, k + Kv4<D>::CODES + warp * C::SCALES, C::SCALES, bar);
+                bulk_load(dst + C::HALF, v + warp * C::CODES, C::CODES, bar);
+                bulk_load(dst + C::HALF + C::CODES, v + Kv4<D>::CODES + warp * C::SCALES, C::SCALES, bar);
+            } else {
+                mbar_arrive(bars + 8 * s);
+            }
         }
-        return true;
     };
-    if (threadIdx.x == 0)
-        for (int t = 0; t < min(n_t, STAGES); ++t) load(t);
-    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i)
+        if (i < n_i) load(i, __ldg(pt + i));
+    int next_page = STAGES < n_i ? __ldg(pt + STAGES) : 0;
 
     {
         // ------------------------------------------------------------------ attention
@@ -143,22 +150,28 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         const int v_a = 2 * c + (c & 1), v_b = v_a ^ 1;     // V pairs: tokens (v_a, v_b) and those + 8
         const float sc = a.scale_log2;
 
-        // Scores (already products) to probabilities: ok0 / ok1 are bit masks over r and e for tokens k_tok and k_tok + 8.
-        auto softmax = [&](float(&s)[R8][4], auto admits, uint32_t(&pf)[R8][2]) {
+        // Scores (products) of GP groups of 16 tokens to probabilities, in fragments for the product with V.  admits(p, r, e): whether the
+        // token of score e (k_tok of group p, + 8 from e = 2 on) counts for row 2 c + (e & 1) of block r.
+        auto softmax = [&](auto &s, auto admits, auto &pf) {
+            constexpr int GP = sizeof(s) / sizeof(s[0]);
             bool move = false;
 #pragma unroll
-            for (int r = 0; r < R8; ++r)
+            for (int p = 0; p < GP; ++p)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[r][e] = admits(r, e) ? s[r][e] * sc : -INFINITY;
-                    move |= s[r][e] > m[r][e & 1] + RESCALE_LOG2;
-                }
+                for (int r = 0; r < R8; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[p][r][e] = admits(p, r, e) ? s[p][r][e] * sc : -INFINITY;
+                        move |= s[p][r][e] > m[r][e & 1] + RESCALE_LOG2;
+                    }
             if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
                 for (int r = 0; r < R8; ++r)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(s[r][e], s[r][e + 2]);
+                        float mx = fmaxf(s[0][r][e], s[0][r][e + 2]);
+#pragma unroll
+                        for (int p = 1; p < GP; ++p) mx = fmaxf(mx, fmaxf(s[p][r][e], s[p][r][e + 2]));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -175,35 +188,36 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     }
             }
 #pragma unroll
-            for (int r = 0; r < R8; ++r) {
-                float p[4];
+            for (int p = 0; p < GP; ++p)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = ex2_approx(s[r][e] - (m[r][e & 1] == -INFINITY ? 0.f : m[r][e & 1]));
-                l[r][0] += p[0] + p[2];
-                l[r][1] += p[1] + p[3];
-                pf[r][0] = movmatrix(pack_bf16x2(p[0], p[1]));
-                pf[r][1] = movmatrix(pack_bf16x2(p[2], p[3]));
-            }
+                for (int r = 0; r < R8; ++r) {
+                    float q[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[e] = ex2_approx(s[p][r][e] - (m[r][e & 1] == -INFINITY ? 0.f : m[r][e & 1]));
+                    l[r][0] += q[0] + q[2];
+                    l[r][1] += q[1] + q[3];
+                    pf[p][r][0] = movmatrix(pack_bf16x2(q[0], q[1]));
+                    pf[p][r][1] = movmatrix(pack_bf16x2(q[2], q[3]));
+                }
         };
 
         bool ok = true;
-        for (int t = 0; t < n_t; ++t) {
-            const int st = t % STAGES;
-            if (threadIdx.x == 0 && t >= LAG && t + STAGES - LAG < n_t) load(t + STAGES - LAG);
-            __syncwarp();
-            ok = mbar_wait(full(st), (t / STAGES) & 1u, abort_flag);
+        for (int i = 0; i < n_i; ++i) {
+            const int st = i % STAGES;
+            ok = mbar_wait(bars + 8 * st, (i / STAGES) & 1u, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const unsigned char *tile = smem + st * C::PAIR;
-            const uint32_t keep = gone[st] ? 0u : 0xffffffffu;
+            const unsigned char *tile = mine + st * C::BYTES;
+            const uint32_t keep = (absent >> st) & 1u ? 0u : 0xffffffffu;
             // ---- S^T = K Q^T
-            float s[R8][4];
+            float s[2][R8][4];
 #pragma unroll
-            for (int r = 0; r < R8; ++r)
+            for (int p = 0; p < 2; ++p) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
-            {
-                const int t0 = 16 * warp + k_tok;
+                for (int r = 0; r < R8; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[p][r][e] = 0.f;
+                const int t0 = 16 * p + k_tok;
                 uint32_t kw[2][C::RUN / 8], s2[2], o2[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -215,34 +229,35 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                         const uint2 x = *reinterpret_cast<const uint2 *>(row);
                         kw[h][0] = x.x, kw[h][1] = x.y;
                     }
-                    const uint32_t sb = tile[Kv4<D>::CODES + (t0 + 8 * h) * Kv4<D>::SROW + (D == 128 ? c : c >> 1)];
+                    const uint32_t sb = tile[C::CODES + (t0 + 8 * h) * Kv4<D>::SROW + (D == 128 ? c : c >> 1)];
                     s2[h] = kv4_scale_pair(sb, sb) & keep;
                     o2[h] = kv4_offset(s2[h]);
                 }
 #pragma unroll
-                for (int i = 0; i < C::RUN / 8; ++i) {
+                for (int j = 0; j < C::RUN / 8; ++j) {
                     uint32_t lo[4], hi[4];
-                    kv4_word(kw[0][i], s2[0], o2[0], lo);
-                    kv4_word(kw[1][i], s2[1], o2[1], hi);
+                    kv4_word(kw[0][j], s2[0], o2[0], lo);
+                    kv4_word(kw[1][j], s2[1], o2[1], hi);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t af[4] = {lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1]};
 #pragma unroll
-                        for (int r = 0; r < R8; ++r) mma_bf16_16816(s[r], af, qf[r][4 * i + 2 * h], qf[r][4 * i + 2 * h + 1]);
+                        for (int r = 0; r < R8; ++r) mma_bf16_16816(s[p][r], af, qf[r][4 * j + 2 * h], qf[r][4 * j + 2 * h + 1]);
                     }
                 }
             }
             // ---- softmax
-            uint32_t pf[R8][2];
-            const int left = L - (t_lo + t) * SPECROLL_PAGE_TOKENS - 16 * warp - k_tok;  // > 0: token k_tok is in the sequence
-            softmax(s, [&](int, int e) { return left > (e & 2 ? 8 : 0); }, pf);
+            uint32_t pf[2][R8][2];
+            const int left = L - (first + i * SPECROLL_PAGE_TOKENS) - k_tok;  // > 0: token k_tok is in the sequence
+            softmax(s, [&](int p, int, int e) { return left > 16 * p + (e & 2 ? 8 : 0); }, pf);
             // ---- O^T += V^T P^T
-            {
-                const unsigned char *vt = tile + Kv4<D>::TILE;
+            const unsigned char *vt = tile + C::HALF;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
                 uint32_t vw[4][C::VRUN / 8], sb[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int tok = 16 * warp + ((q & 1) ? v_b : v_a) + 8 * (q >> 1);
+                    const int tok = 16 * p + ((q & 1) ? v_b : v_a) + 8 * (q >> 1);
                     const unsigned char *row = vt + tok * Kv4<D>::ROW + (C::VRUN / 2) * g;
                     if constexpr (D == 128) {
                         const uint2 x = *reinterpret_cast<const uint2 *>(row);
@@ -250,36 +265,39 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     } else {
                         vw[q][0] = *reinterpret_cast<const uint32_t *>(row);
                     }
-                    sb[q] = vt[Kv4<D>::CODES + tok * Kv4<D>::SROW + (g * C::VRUN) / 32];
+                    sb[q] = vt[C::CODES + tok * Kv4<D>::SROW + (g * C::VRUN) / 32];
                 }
                 const uint32_t s0 = kv4_scale_pair(sb[0], sb[1]) & keep, s1 = kv4_scale_pair(sb[2], sb[3]) & keep;
                 const uint32_t f0 = kv4_offset(s0), f1 = kv4_offset(s1);
 #pragma unroll
-                for (int i = 0; i < C::VRUN / 8; ++i) {
+                for (int j = 0; j < C::VRUN / 8; ++j) {
                     // lower halves: elements 0 2 4 6 of the word, upper halves: 1 3 5 7, of two tokens each
                     uint32_t e0_[4], e1_[4], d0_[4], d1_[4];
-                    kv4_word(__byte_perm(vw[0][i], vw[1][i], 0x5410), s0, f0, e0_);
-                    kv4_word(__byte_perm(vw[0][i], vw[1][i], 0x7632), s0, f0, d0_);
-                    kv4_word(__byte_perm(vw[2][i], vw[3][i], 0x5410), s1, f1, e1_);
-                    kv4_word(__byte_perm(vw[2][i], vw[3][i], 0x7632), s1, f1, d1_);
+                    kv4_word(__byte_perm(vw[0][j], vw[1][j], 0x5410), s0, f0, e0_);
+                    kv4_word(__byte_perm(vw[0][j], vw[1][j], 0x7632), s0, f0, d0_);
+                    kv4_word(__byte_perm(vw[2][j], vw[3][j], 0x5410), s1, f1, e1_);
+                    kv4_word(__byte_perm(vw[2][j], vw[3][j], 0x7632), s1, f1, d1_);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t af[4] = {e0_[j], d0_[j], e1_[j], d1_[j]};
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t af[4] = {e0_[q], d0_[q], e1_[q], d1_[q]};
 #pragma unroll
-                        for (int r = 0; r < R8; ++r) mma_bf16_16816(o[r][4 * i + j], af, pf[r][0], pf[r][1]);
+                        for (int r = 0; r < R8; ++r) mma_bf16_16816(o[r][4 * j + q], af, pf[p][r][0], pf[p][r][1]);
                     }
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(empty(st));
+            if (i + STAGES < n_i) {
+                load(i + STAGES, next_page);
+                next_page = i + STAGES + 1 < n_i ? __ldg(pt + i + STAGES + 1) : 0;
+            }
         }
         if (ok && has_tree && 16 * warp < N) {
             // ---- the tree's rows, bf16 from global memory, sixteen nodes a warp
-            float s[R8][4];
+            float s[1][R8][4];
 #pragma unroll
             for (int r = 0; r < R8; ++r)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
+                for (int e = 0; e < 4; ++e) s[0][r][e] = 0.f;
             const size_t rows_of_b = (size_t)b * N;
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
             uint4 kx[2][C::RUN / 8];
@@ -298,12 +316,12 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t af[4] = {lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1]};
 #pragma unroll
-                    for (int r = 0; r < R8; ++r) mma_bf16_16816(s[r], af, qf[r][4 * i + 2 * h], qf[r][4 * i + 2 * h + 1]);
+                    for (int r = 0; r < R8; ++r) mma_bf16_16816(s[0][r], af, qf[r][4 * i + 2 * h], qf[r][4 * i + 2 * h + 1]);
                 }
             }
-            uint32_t pf[R8][2];
+            uint32_t pf[1][R8][2];
             const int n0 = 16 * warp + k_tok;
-            softmax(s, [&](int r, int e) {
+            softmax(s, [&](int, int r, int e) {
                 const int gr = row0 + 8 * r + 2 * c + (e & 1);
                 return gr < a.rows && ((mask.anc[gr / G] >> (n0 + (e & 2 ? 8 : 0))) & 1ull);
             }, pf);
@@ -324,7 +342,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     const uint32_t af[4] = {__byte_perm(x[0][j], x[1][j], 0x5410), __byte_perm(x[0][j], x[1][j], 0x7632),
                                             __byte_perm(x[2][j], x[3][j], 0x5410), __byte_perm(x[2][j], x[3][j], 0x7632)};
 #pragma unroll
-                    for (int r = 0; r < R8; ++r) mma_bf16_16816(o[r][4 * i + j], af, pf[r][0], pf[r][1]);
+                    for (int r = 0; r < R8; ++r) mma_bf16_16816(o[r][4 * i + j], af, pf[0][r][0], pf[0][r][1]);
                 }
             }
         }
@@ -410,6 +428,91 @@ static int launch_kv4(const AttnArgs &a, const TopoMask &mask, int32_t *status, 
     const int rc = device_setup(reinterpret_cast<const void *>(kern), C::SMEM, nullptr);
     if (rc != SPECROLL_OK) return rc;
     SR_CUDA_TRY(launch_dependent(!a.no_pdl, kern, dim3((unsigned)a.total_work), dim3(akv4::THREADS), C::SMEM, st, a, mask, status));
+    return SPECROLL_OK;
+}
+
+// Sums the chunks of every split sequence.  grid = (B, Hkv, 4): a block has a quarter of D of all rows of one (sequence, KV head), 4 D floats
+// of which a thread takes four, and as many parts of the chunks as 256 threads have room for; a part's chunks are taken eight at a
+// time with all their loads in flight.  Launched as a programmatic dependent of the attention kernel; the plan is complete when it starts.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
+    constexpr int COLS = D / 16, ITEMS = ROWS * COLS, PARTS = 256 / ITEMS, STEP = 8;
+    static_assert(PARTS >= 1 && PARTS * ITEMS == 256, "whole blocks");
+    __shared__ float2 sh_ml[256];
+    __shared__ float4 sh_acc[256];
+    pdl_launch_dependents();
+    const int b = blockIdx.x, hkv = blockIdx.y, part = threadIdx.x / ITEMS, row = threadIdx.x % ROWS, d4 = blockIdx.z * COLS + threadIdx.x % ITEMS / ROWS;
+    const int item0 = __ldcg(a.item_start + b), n_splits = __ldcg(a.item_start + b + 1) - item0;
+    if (n_splits < 2) return;
+    pdl_wait();
+    for (int rb = 0; rb < a.n_rb; ++rb) {
+        const int gr = rb * ROWS + row;
+        const size_t unit = (size_t)item0 * a.Hkv + hkv;
+        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + unit * a.rows_pad + gr;
+        const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + (unit * (D / 4) + d4) * a.rows_pad + gr;
+        const size_t step_ml = (size_t)a.Hkv * a.rows_pad, step_o = step_ml * (D / 4);
+        float M = -INFINITY, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int i0 = part; i0 < n_splits; i0 += STEP * PARTS) {
+            float2 v[STEP];
+            float4 x[STEP];
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                const size_t s = (size_t)min(i0 + i * PARTS, n_splits - 1);  // (a chunk beyond the last: weight zero below)
+                v[i] = __ldcg(ml + s * step_ml);
+                x[i] = __ldcg(po + s * step_o);
+            }
+            float top = M;
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) top = fmaxf(top, v[i].x);
+            const float f = M == -INFINITY ? 0.f : ex2_approx(M - top);
+            M = top;
+            sum *= f;
+            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                const float w = (i0 + i * PARTS >= n_splits || v[i].x == -INFINITY) ? 0.f : ex2_approx(v[i].x - M);
+                sum += w * v[i].y;
+                acc.x += w * x[i].x;
+                acc.y += w * x[i].y;
+                acc.z += w * x[i].z;
+                acc.w += w * x[i].w;
+            }
+        }
+        sh_ml[threadIdx.x] = make_float2(M, sum);
+        sh_acc[threadIdx.x] = acc;
+        __syncthreads();
+        if (part == 0 && gr < a.rows) {
+#pragma unroll
+            for (int q = 1; q < PARTS; ++q) M = fmaxf(M, sh_ml[q * ITEMS + threadIdx.x].x);
+            sum = 0.f;
+            acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) {
+                const float2 e = sh_ml[q * ITEMS + threadIdx.x];
+                const float4 y = sh_acc[q * ITEMS + threadIdx.x];
+                const float w = e.x == -INFINITY ? 0.f : ex2_approx(e.x - M);
+                sum += w * e.y;
+                acc.x += w * y.x;
+                acc.y += w * y.y;
+                acc.z += w * y.z;
+                acc.w += w * y.w;
+            }
+            const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+            const size_t at = ((size_t)b * a.N + gr / a.G) * a.Hq + hkv * a.G + gr % a.G;
+            *reinterpret_cast<uint2 *>(a.O + at * D + 4 * d4) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+            if (a.lse && d4 == 0) a.lse[at] = (M + log2f(sum)) * 0.6931471805599453f;
+        }
+        __syncthreads();
+    }
+}
+
+int launch_attn_merge_kv4(const AttnArgs &a, int D, cudaStream_t st) {
+    const bool one = a.rows_per_block == 8;
+    auto *const kern = D == 128 ? (one ? attn_merge_kv4_kernel<128, 8> : attn_merge_kv4_kernel<128, 16>)
+                                : (one ? attn_merge_kv4_kernel<64, 8> : attn_merge_kv4_kernel<64, 16>);
+    SR_CUDA_TRY(launch_dependent(!a.no_pdl, kern, dim3((unsigned)a.B, (unsigned)a.Hkv, 4), dim3(256), 0, st, a));
     return SPECROLL_OK;
 }
 

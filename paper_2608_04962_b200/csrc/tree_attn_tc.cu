@@ -67,13 +67,20 @@ struct Cfg {
     // three stages each for that, which does not fit beside two Q buffers.
     static constexpr int RS = KV4 ? 4 : 5;   // ring stages
     // 4-bit cache: K and V of a page arrive as codes in SS staging slots; four warps decode them into the ring's stages
-    static constexpr int SS = KV4 ? 3 : 0, SLOT_BYTES = KV4 ? Kv4<D>::TILE : 0, DECODE_WARPS = KV4 ? 4 : 0;
+    static constexpr int SS = KV4 ? 3 : 0, SLOT_BYTES = KV4 ? Kv4<D>::TILE : 0, DECODE_WARPS = KV4 ? 4 : 0, DECODE_TEAMS = KV4 ? 2 : 0;
+    // Job n is in slot n mod SS and is told on barrier n mod SF, which only one team waits for: it has then seen every phase before.
+    static constexpr int SF = SS * DECODE_TEAMS;
     static constexpr int QS = 2;   // Q buffers (units)
     static constexpr int MMA_WARPS = 2;  // issuing threads (one lane of each)
     static constexpr int SOFTMAX_THREADS = 256, OUT_THREADS = 128;
     // first warps of the softmax, output and decoding roles (whole groups of four where there is decoding)
     static constexpr int SOFT0 = KV4 ? 4 : 1 + MMA_WARPS, OUT0 = SOFT0 + SOFTMAX_THREADS / 32, DECODE0 = OUT0 + OUT_THREADS / 32;
-    static constexpr int THREADS = 32 * (DECODE0 + DECODE_WARPS);
+    static constexpr int THREADS = 32 * (DECODE0 + DECODE_TEAMS * DECODE_WARPS);
+    // Registers a thread of each role, where there is decoding: 768 threads get 80 each at the launch, and the groups of four warps share
+    // the same sum out anew (the softmax threads keep a tile's probabilities in registers).
+    static constexpr int REGS_LOAD = 56, REGS_SOFT = 120, REGS_OUT = 72, REGS_DECODE = 56;
+    static_assert(!KV4 || REGS_LOAD + REGS_SOFT * (SOFTMAX_THREADS / 128) + REGS_OUT + REGS_DECODE * DECODE_TEAMS == 80 * (THREADS / 128),
+                  "no more registers than the launch gave");
     static constexpr int FULL_ARRIVALS = KV4 ? DECODE_WARPS : 1;  // of a ring stage: the decoding warps, or the loading thread
     static constexpr int Q_BYTES = NBOX * BOX_BYTES;   // the Q block of one unit
     static constexpr int KV_BYTES = NBOX * BOX_BYTES;  // one K tile or one V tile
@@ -82,7 +89,7 @@ struct Cfg {
                          B_PVDONE = B_PREADY + SB, B_QFULL = B_PVDONE + SB, B_QFREE = B_QFULL + QS,
                          B_UFULL = B_QFREE + QS, B_UEMPTY = B_UFULL + 2, B_X = B_UEMPTY + 2, B_ALL = B_X + 4,
                          B_OFULL = B_ALL + 1, B_OFREE = B_OFULL + 1, B_HFULL = B_OFREE + 1, B_HFREE = B_HFULL + 1,
-                         B_SFILLED = B_HFREE + 1, B_SFREE = B_SFILLED + SS, N_BARS = B_SFREE + SS;
+                         B_SFILLED = B_HFREE + 1, B_SFREE = B_SFILLED + SF, N_BARS = B_SFREE + SS;
     static constexpr int BAR_BYTES = (8 * N_BARS + 15) / 16 * 16;
     // exchange area: the rows' reference maxima as one softmax team leaves them for the other ([2][128] fp32), or
     // the partial row maxima of the pairs (per lane group [2 slots][2 halves][32 lanes] bf16)
@@ -141,11 +148,13 @@ __device__ __forceinline__ float bf16_bits_to_float(unsigned short b) { return _
 // ONE: every CTA has one unit at most (few sequences): the second Q buffer is free for the hand-over area, and nothing is
 // counted - the merge, if any, is a kernel of its own - so the CTA leaves without a round trip to memory.  (A template flag:
 // asked at run time it cost the shapes with many units 1-4 %.)
-// KV4: the cache is a 4-bit paged pool (tmK and tmV are not used).  Pages come as codes into staging slots by untiled bulk copies; four
-// warps more take the slots in order and decode them into the ring's stages, in the 128-byte swizzle that TMA would have left.  The
-// tree's tiles go through the same queue, as a slot that names the tile, and are fetched into their stages from there: the ring's
-// stages are filled by the decoding warps alone, in one order, so that a stage's barrier is never a phase further behind than its parity
-// can tell.
+// KV4: the cache is a 4-bit paged pool (tmK and tmV are not used).  Pages come as codes into staging slots by untiled bulk copies; two
+// teams of four warps take the slots in turn and decode them into the ring's stages, in the 128-byte swizzle that TMA would have left.
+// The tree's tiles go through the same queue, as a slot that names the tile, and are fetched into their stages from there, so that
+// stages are filled by the decoding teams alone.  A wait on a barrier's parity is right while the waiter is at most one phase behind or
+// ahead: a stage's job waits for the stage's use before to be consumed, so that use's own job must not be still waiting for the
+// one before it.  With SS = 3 slots only two neighbouring jobs of the queue can be in the teams' hands at a time (the one after them needs a slot that
+// the first still holds), and neighbours never have positions four apart but at the very start (K1 V1), where there is no use before.
 template <int D, bool TEAMS, bool ONE, bool KV4>
 __global__ void __launch_bounds__(attc::Cfg<D, TEAMS, KV4>::THREADS, 1)
 tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -251,6 +260,13 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     }
 
+    if constexpr (KV4) {  // (whole groups of four warps; those that give come first, those that take wait for them)
+        if (warp < C::SOFT0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_LOAD));
+        else if (warp < C::OUT0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS_SOFT));
+        else if (warp >= C::DECODE0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_DECODE));
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_OUT));
+    }
+
     // Sums the partials of all chunks of one (sequence, kv head, row block) for columns [col0, col0 + ncols) of one row;
     // run by the threads that own the row block, after the tickets showed that every chunk has been written.
     auto merge_rows = [&](int b, int hkv, int rb, int n_splits, int item0, int row, int col0, int ncols) {
@@ -316,12 +332,14 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             int n_pend = 0;
             // 4-bit cache: the job for ring position pos (codes of a page: K where kind is TREE_K, else V; or the tree's tile) into the next slot
             uint32_t staged = 0;
+            auto filled = [&]() { return bar(C::B_SFILLED + (int)(staged % (C::SF ? C::SF : 1))); };
             auto slot_free = [&]() { return bar(C::B_SFREE + (int)(staged % (C::SS ? C::SS : 1))); };
             auto slot_parity = [&]() { return ((staged / (C::SS ? C::SS : 1)) & 1u) ^ 1u; };
             auto post = [&](bool tree, int kind, int hkv, int at, uint32_t pos) -> bool {
                 if constexpr (KV4) {
                     const int s = (int)(staged % C::SS);
                     if (!twait(5, slot_free(), slot_parity())) return false;
+                    const uint32_t told = filled();
                     ++staged;
                     const bool codes = !tree && at >= 0 && at < a.n_pages;
                     slot_job[4 * s] = (int)pos;
@@ -329,11 +347,11 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     slot_job[4 * s + 2] = hkv;
                     slot_job[4 * s + 3] = at;
                     if (codes) {
-                        mbar_arrive_expect_tx(bar(C::B_SFILLED + s), C::SLOT_BYTES);
+                        mbar_arrive_expect_tx(told, C::SLOT_BYTES);
                         bulk_load(g_s + s * C::SLOT_BYTES, a.pool + (((size_t)at * a.Hkv + hkv) * 2 + (kind == TREE_V)) * C::SLOT_BYTES,
-                                  C::SLOT_BYTES, bar(C::B_SFILLED + s));
+                                  C::SLOT_BYTES, told);
                     } else {
-                        mbar_arrive(bar(C::B_SFILLED + s));
+                        mbar_arrive(told);
                     }
                 }
                 return true;
@@ -488,10 +506,13 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             // flush the V tiles still pending (the last two tiles of the last unit)
             for (int i = 0; i < n_pend && ok; ++i) ok = load_v(pv_map[i], pv_h[i], pv_tok[i]);
             if constexpr (KV4) {
-                const int s = (int)(staged % C::SS);
-                if (ok && (ok = twait(6, slot_free(), slot_parity()))) {
+                for (int i = 0; i < C::DECODE_TEAMS && ok; ++i) {  // the end, once for each team
+                    const int s = (int)(staged % C::SS);
+                    ok = twait(6, slot_free(), slot_parity());
+                    if (!ok) break;
                     slot_job[4 * s] = -1;
-                    mbar_arrive(bar(C::B_SFILLED + s));
+                    mbar_arrive(filled());
+                    ++staged;
                 }
             }
             if (!ok) {
@@ -597,17 +618,24 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     } else if (warp < C::SOFT0) {
         // (fills the group of four)
     } else if (KV4 && warp >= C::DECODE0) {
-        // ------------------------------------------------------------------ codes to bf16 (4 warps)
+        // ------------------------------------------------------------------ codes to bf16 (8 warps)
         // A warp has 8 (D = 128) or 16 tokens at a time, a thread one block of 32 elements: 16 bytes of codes, one scale, four 16-byte
-        // chunks of the stage.  Threads of a token's second box take their chunks in another order, so that eight neighbouring threads
-        // write eight different bank groups.
+        // chunks of the stage.  Of eight neighbouring threads, whose stores are one wavefront, two have the blocks of one 128-byte row of the
+        // stage and four neighbouring tokens, so that the swizzle sends them to eight different bank groups.
         if constexpr (KV4) {
-            constexpr int PER = D / 32, STEP = 32 / PER;  // threads of a token, tokens of a warp's step
-            const int dw = warp - C::DECODE0, c = lane % PER, flip = D == 128 ? (c >> 1) * 2 : 0;
+            constexpr int STEP = 1024 / D;  // tokens of a warp's step
+            const int dw = (warp - C::DECODE0) % C::DECODE_WARPS;
+            const int c = D == 128 ? (lane & 1) | ((lane >> 2) & 2) : lane & 1;                     // block of the token
+            const int tw = D == 128 ? ((lane >> 1) & 3) | ((lane >> 2) & 4) : lane >> 1;            // token of the step
+            const uint32_t off0 = (D == 128 ? (uint32_t)(c >> 1) * BOX_BYTES : 0u) + (uint32_t)(dw * STEP + tw) * 128u;
+            uint32_t off[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) off[i] = off0 + ((uint32_t)((c & 1) * 4 + i) ^ (uint32_t)(tw & 7)) * 16u;
+            const int code0 = (dw * STEP + tw) * Kv4<D>::ROW + 16 * c, scale0 = Kv4<D>::CODES + (dw * STEP + tw) * Kv4<D>::SROW + c;
             bool ok = true;
-            for (uint32_t n = 0; ok; ++n) {
+            for (uint32_t n = (uint32_t)((warp - C::DECODE0) / C::DECODE_WARPS); ok; n += C::DECODE_TEAMS) {
                 const int s = (int)(n % C::SS);
-                ok = twait(0, bar(C::B_SFILLED + s), (n / C::SS) & 1u);
+                ok = twait(0, bar(C::B_SFILLED + (int)(n % C::SF)), (n / C::SF) & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 const int pos = slot_job[4 * s], kind = slot_job[4 * s + 1];
@@ -634,22 +662,28 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     continue;
                 }
                 const unsigned char *codes = aligned + QS * C::Q_BYTES + RS * C::KV_BYTES + s * C::SLOT_BYTES;
-                const uint32_t dst = stage_addr(st) + (D == 128 ? (uint32_t)(c >> 1) * BOX_BYTES : 0u);
                 const uint32_t keep = kind == CODES ? 0xffffffffu : 0u;  // (no such page: zeros)
+                // (all loads ahead of the first store: the compiler may not move them across one)
+                constexpr int STEPS = BN / (C::DECODE_WARPS * STEP), TOKENS = C::DECODE_WARPS * STEP;
+                uint4 w[STEPS];
+                uint32_t sb[STEPS], dst[4];
 #pragma unroll
-                for (int it = 0; it < BN / (4 * STEP); ++it) {
-                    const int tok = (it * 4 + dw) * STEP + lane / PER;
-                    const uint4 w = *reinterpret_cast<const uint4 *>(codes + tok * Kv4<D>::ROW + 16 * c);
-                    const uint32_t sb = codes[Kv4<D>::CODES + tok * Kv4<D>::SROW + c];
-                    const uint32_t s2 = kv4_scale_pair(sb, sb) & keep, o2 = kv4_offset(s2);
-                    const uint32_t ww[4] = {flip ? w.z : w.x, flip ? w.w : w.y, flip ? w.x : w.z, flip ? w.y : w.w};
-                    const uint32_t row = dst + (uint32_t)tok * 128u;
+                for (int it = 0; it < STEPS; ++it) {
+                    w[it] = *reinterpret_cast<const uint4 *>(codes + code0 + it * TOKENS * Kv4<D>::ROW);
+                    sb[it] = codes[scale0 + it * TOKENS * Kv4<D>::SROW];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dst[i] = stage_addr(st) + off[i];
+#pragma unroll
+                for (int it = 0; it < STEPS; ++it) {
+                    const uint32_t s2 = kv4_scale_pair(sb[it], sb[it]) & keep, o2 = kv4_offset(s2);
+                    const uint32_t ww[4] = {w[it].x, w[it].y, w[it].z, w[it].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t r[4];
                         kv4_word(ww[i], s2, o2, r);
-                        const uint32_t chunk = (uint32_t)((c & 1) * 4 + (i ^ flip)) ^ (uint32_t)(tok & 7);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + chunk * 16u), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst[i] + (uint32_t)(it * TOKENS * 128)), "r"(r[0]),
+                                     "r"(r[1]), "r"(r[2]), "r"(r[3])
                                      : "memory");
                     }
                 }
@@ -1214,6 +1248,15 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     // ------------------------------------------------------------------ teardown
     tc_fence_before();
     __syncthreads();
+    if constexpr (KV4) {
+        // aborting: what is in flight (copies, also of the decoding warps, and tensor operations) gets time to land before TMEM and the CTA go
+        if (*abort_flag) {
+            const unsigned long long t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 20000000ull) {
+            }
+            __syncthreads();
+        }
+    }
     if (threadIdx.x == 0) {
         if (*abort_flag) {
             // status word 1: index of the barrier whose wait ran out, parity in bit 8 (diagnostic only)
