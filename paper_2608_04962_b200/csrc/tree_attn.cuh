@@ -8,7 +8,7 @@ namespace specroll {
 struct AttnArgs {
     const __nv_bfloat16 *Q, *Kc, *Vc, *Kt, *Vt;
     const int32_t *kv_indptr;
-    const int32_t *item_start;  // [B+1] exclusive prefix of the per-sequence chunk counts (sequence order)
+    int32_t *item_start;  // [B+1] exclusive prefix of the per-sequence chunk counts (sequence order)
     __nv_bfloat16 *O;
     float *lse;
     float *part_o;   // [items, Hkv, rows_pad, D]   un-normalised partial outputs of split sequences
@@ -34,6 +34,8 @@ struct AttnArgs {
     int32_t kv4;                  // the cache is one
     const uint8_t *pool;          // u8 [n_pages][Hkv][2][tile]
     int32_t n_pages;
+    const int32_t *kv_len, *page_indptr;  // tree_attn_kv4.cu finds its units itself
+    int32_t items;                // chunks that the host counted
     int32_t no_pdl;               // launch the attention kernel as an ordinary kernel, not as a programmatic dependent
 };
 

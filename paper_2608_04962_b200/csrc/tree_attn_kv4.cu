@@ -10,8 +10,8 @@
 // contiguous: for K a thread has 1/4 of a token's elements (one scale block where D = 128), for V 1/8 of four tokens' elements,
 // paired by byte permutes before decoding.  Tokens of a pair change places in every other pair, which halves the bank conflicts
 // of V's reads.
-// Every warp has a softmax of its own (reference maximum per row, moved only when a score exceeds it by 2^8); the four meet in
-// shared memory at the end.  The tree's bf16 rows are done by the warps after their slices, sixteen nodes each.
+// Every warp has a softmax of its own (reference maximum per row, which stays until a score is 2^8 above it); the four meet in
+// shared memory at the end.  The tree's bf16 rows are done by the warps before their slices, sixteen nodes each.
 // What bounds it: 17 KB of a page in 0.4 us at the HBM rate of one SM, against some 600 issue slots a scheduler for decoding it.
 #include <math.h>
 
@@ -25,7 +25,6 @@ namespace akv4 {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int SLICE = 32, PER_PAGE = SPECROLL_PAGE_TOKENS / SLICE;  // tokens a warp fetches and takes at a time
 constexpr int STAGES = 3;
-constexpr float RESCALE_LOG2 = 8.0f;
 
 template <int D, int R8>
 struct Cfg {
@@ -70,14 +69,60 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     pdl_wait();
     pdl_launch_dependents();
 
-    // ---- the unit: (chunk in work order, KV head, row block)
-    int w = blockIdx.x;
-    const int rb = w % a.n_rb;
-    w /= a.n_rb;
-    const int hkv = w % a.Hkv, si = w / a.Hkv;
-    const int4 e0 = __ldg(reinterpret_cast<const int4 *>(a.unit_tab) + 2 * (size_t)si);
-    const int4 e1 = __ldg(reinterpret_cast<const int4 *>(a.unit_tab) + 2 * (size_t)si + 1);
-    const int b = e0.x, split = e0.y, n_splits = e0.z, item = e0.w + split, slot0 = e1.x, L = e1.y;
+    // ---- the unit: (chunk, KV head, row block).  Chunks are counted in the order of the sequences; every CTA finds its own from the
+    // lengths (a plan made by a kernel in front took ten microseconds for 256 sequences).
+    if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;  // (seconds ahead of any wait that could run out)
+    const int rb = (int)blockIdx.x % a.n_rb, hkv = (int)blockIdx.x / a.n_rb % a.Hkv, item = (int)blockIdx.x / a.n_rb / a.Hkv;
+    {
+        volatile int *const found = reinterpret_cast<volatile int *>(smem);  // [0..5]: the unit, [8 ..]: chunks of the warps' sequences
+        const int per = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
+        auto chunks = [&](int len) { return max(1, ((len + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS + a.chunk_tiles - 1) / a.chunk_tiles); };
+        // (lengths four at a time, so that their loads are under way together; the first four sequences' pages as well)
+        int own = 0, pages[4];
+        for (int i = b0; i < b1; i += 4) {
+            int len[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) len[q] = i + q < b1 ? __ldg(a.kv_len + i + q) : 0;
+            if (i == b0) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) pages[q] = i + q < b1 ? __ldg(a.page_indptr + i + q) : 0;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) own += i + q < b1 ? chunks(max(len[q], 0)) : 0;
+        }
+        int sum = own;
+#pragma unroll
+        for (int o_ = 1; o_ < 32; o_ <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, sum, o_);
+            if (lane >= o_) sum += x;
+        }
+        if (lane == 31) found[8 + warp] = sum;
+        if (threadIdx.x == 0) found[0] = -1;
+        __syncthreads();
+        int at = sum - own;
+#pragma unroll
+        for (int q = 0; q < WARPS - 1; ++q) at += q < warp ? found[8 + q] : 0;
+        if (item >= at && item < at + own) {
+            for (int i = b0; i < b1; ++i) {
+                const int len = max(__ldg(a.kv_len + i), 0), ns = chunks(len);
+                if (item < at + ns) {
+                    found[0] = i;
+                    found[1] = item - at;
+                    found[2] = ns;
+                    found[3] = len;
+                    found[4] = i - b0 == 0 ? pages[0] : i - b0 == 1 ? pages[1] : i - b0 == 2 ? pages[2] : i - b0 == 3 ? pages[3] : __ldg(a.page_indptr + i);
+                    if (item == at && hkv == 0 && rb == 0) a.item_start[i] = at;  // (for the merge)
+                    break;
+                }
+                at += ns;
+            }
+        }
+        __syncthreads();
+    }
+    const volatile int *const unit_s = reinterpret_cast<const volatile int *>(smem);
+    const int b = unit_s[0], split = unit_s[1], n_splits = unit_s[2], L = unit_s[3], slot0 = unit_s[4];
+    __syncthreads();
+    if (b < 0) return;  // (lengths that make fewer chunks than the host's)
     const int tiles_b = (L + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS;
     const int tps = (tiles_b + n_splits - 1) / n_splits;
     const int t_lo = min(tiles_b, split * tps), n_t = min(tiles_b, t_lo + tps) - t_lo;
@@ -88,43 +133,43 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     const int n_i = end > first ? (end - first + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS : 0;
 
     float o[R8][C::MB][4];
-    float m[R8][2], l[R8][2];
+    float m[R8][2], ref[R8][2], l[R8][2];  // reference maxima (ref: the same, but 0 where there is none yet) and sums
 #pragma unroll
     for (int r = 0; r < R8; ++r) {
         m[r][0] = m[r][1] = -INFINITY;
-        l[r][0] = l[r][1] = 0.f;
+        l[r][0] = l[r][1] = ref[r][0] = ref[r][1] = 0.f;
 #pragma unroll
         for (int i = 0; i < C::MB; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[r][i][e] = 0.f;
     }
 
-    // ---- loads: slice i into stage i mod STAGES, by the warp's first thread.  A page that does not exist is not fetched: its bit in
-    // `absent` makes the decoded values zeros.
+    // ---- loads: slice i into stage i mod STAGES, by the warp's first thread.  A page that does not exist is not fetched: the warp writes
+    // codes that stand for zero (whatever the scale) in its place.
     const int32_t *const pt = a.page_table + slot0 + t_lo;
-    uint32_t absent = 0u;
     auto load = [&](int i, int page) {
         const int s = i % STAGES;
-        const bool there = page >= 0 && page < a.n_pages;
-        absent = there ? absent & ~(1u << s) : absent | (1u << s);
-        if (lane == 0) {
-            if (there) {
-                const uint32_t dst = smem_u32(mine) + s * C::BYTES, bar = bars + 8 * s;
-                const uint8_t *k = a.pool + ((size_t)page * a.Hkv + hkv) * (2 * Kv4<D>::TILE), *v = k + Kv4<D>::TILE;
+        const uint32_t bar = bars + 8 * s;
+        if (page >= 0 && page < a.n_pages) {
+            if (lane == 0) {
+                const uint32_t dst = smem_u32(mine) + s * C::BYTES;
+                const uint8_t *k = a.pool + ((size_t)page * a.Hkv + hkv) * (2 * Kv4<D>::TILE) + warp * C::CODES;
+                const uint8_t *ks = k + Kv4<D>::CODES - warp * (C::CODES - C::SCALES);
                 mbar_arrive_expect_tx(bar, C::BYTES);
-                bulk_load(dst, k + warp * C::CODES, C::CODES, bar);
-                bulk_load(dst + C::CODES, k + Kv4<D>::CODES + warp * C::SCALES, C::SCALES, bar);
-                bulk_load(dst + C::HALF, v + warp * C::CODES, C::CODES, bar);
-                bulk_load(dst + C::HALF + C::CODES, v + Kv4<D>::CODES + warp * C::SCALES, C::SCALES, bar);
-            } else {
-                mbar_arrive(bars + 8 * s);
+                bulk_load(dst, k, C::CODES, bar);
+                bulk_load(dst + C::CODES, ks, C::SCALES, bar);
+                bulk_load(dst + C::HALF, k + Kv4<D>::TILE, C::CODES, bar);
+                bulk_load(dst + C::HALF + C::CODES, ks + Kv4<D>::TILE, C::SCALES, bar);
             }
+        } else {
+            for (int j = lane; j < C::BYTES / 4; j += 32) reinterpret_cast<uint32_t *>(mine + s * C::BYTES)[j] = 0x88888888u;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
         }
     };
+    int page[STAGES + 1];
 #pragma unroll
-    for (int i = 0; i < STAGES; ++i)
-        if (i < n_i) load(i, __ldg(pt + i));
-    int next_page = STAGES < n_i ? __ldg(pt + STAGES) : 0;
+    for (int i = 0; i <= STAGES; ++i) page[i] = i < n_i ? __ldg(pt + i) : -1;
 
     {
         // ------------------------------------------------------------------ attention
@@ -145,39 +190,92 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 qf[r][4 * i + 3] = x.w;
             }
         }
+        // the tree's rows of this warp, bf16, sixteen nodes: K rows and V rows as the codes of the cache are divided among the threads
+        const bool tree = has_tree && 16 * warp < N;
+        uint4 kx[2][C::RUN / 8], vx[4][C::VRUN / 8];
         // the tokens (of 16) that a thread's indexes stand for: index 2 j + e is token 2 j + (e ^ (j & 1))
         const int k_tok = g ^ ((g >> 1) & 1);               // K rows g and g + 8: tokens k_tok and k_tok + 8
         const int v_a = 2 * c + (c & 1), v_b = v_a ^ 1;     // V pairs: tokens (v_a, v_b) and those + 8
         const float sc = a.scale_log2;
+        if (tree) {
+            const size_t rows_of_b = (size_t)b * N;
+            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = 16 * warp + k_tok + 8 * h;
+                const uint4 *src = reinterpret_cast<const uint4 *>(a.Kt + ((rows_of_b + n) * a.Hkv + hkv) * D + C::RUN * c);
+#pragma unroll
+                for (int i = 0; i < C::RUN / 8; ++i) kx[h][i] = n < N ? __ldg(src + i) : zero;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = 16 * warp + ((q & 1) ? v_b : v_a) + 8 * (q >> 1);
+                const uint4 *src = reinterpret_cast<const uint4 *>(a.Vt + ((rows_of_b + n) * a.Hkv + hkv) * D + C::VRUN * g);
+#pragma unroll
+                for (int i = 0; i < C::VRUN / 8; ++i) vx[q][i] = n < N ? __ldg(src + i) : zero;
+            }
+        }
+        // (the page numbers are there by now; the first pages arrive while the tree is worked on)
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i)
+            if (i < n_i) load(i, page[i]);
+        int next_page = page[STAGES];
 
         // Scores (products) of GP groups of 16 tokens to probabilities, in fragments for the product with V.  admits(p, r, e): whether the
-        // token of score e (k_tok of group p, + 8 from e = 2 on) counts for row 2 c + (e & 1) of block r.
-        auto softmax = [&](auto &s, auto admits, auto &pf) {
+        // token of score e (k_tok of group p, + 8 from e = 2 on) counts for row 2 c + (e & 1) of block r; `whole`: they all do.
+        // The exponentials are taken against the references as they stand, and a row's sum is the alarm for one that has to move: a
+        // score 2^8 above it makes the sum exceed 2^8.
+        auto softmax = [&](auto &s, bool start, bool whole, auto admits, auto &pf) {
             constexpr int GP = sizeof(s) / sizeof(s[0]);
-            bool move = false;
+            float q[GP][R8][4], sum[R8][2];
+            auto exps = [&]() {
 #pragma unroll
-            for (int p = 0; p < GP; ++p)
+                for (int p = 0; p < GP; ++p)
+#pragma unroll
+                    for (int r = 0; r < R8; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) q[p][r][e] = ex2_approx(fmaf(s[p][r][e], sc, -ref[r][e & 1]));
+                if (!whole) {
+#pragma unroll
+                    for (int p = 0; p < GP; ++p)
+#pragma unroll
+                        for (int r = 0; r < R8; ++r)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (!admits(p, r, e)) q[p][r][e] = 0.f;
+                }
 #pragma unroll
                 for (int r = 0; r < R8; ++r)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[p][r][e] = admits(p, r, e) ? s[p][r][e] * sc : -INFINITY;
-                        move |= s[p][r][e] > m[r][e & 1] + RESCALE_LOG2;
+                    for (int e = 0; e < 2; ++e) {
+                        sum[r][e] = q[0][r][e] + q[0][r][e + 2];
+#pragma unroll
+                        for (int p = 1; p < GP; ++p) sum[r][e] += q[p][r][e] + q[p][r][e + 2];
                     }
+            };
+            bool move = start;
+            if (!start) {
+                exps();
+#pragma unroll
+                for (int r = 0; r < R8; ++r) move |= !(fmaxf(sum[r][0], sum[r][1]) <= 256.0f) || !(sum[r][0] + sum[r][1] <= 512.0f);
+            }
             if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
                 for (int r = 0; r < R8; ++r)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(s[0][r][e], s[0][r][e + 2]);
+                        float mx = -INFINITY;
 #pragma unroll
-                        for (int p = 1; p < GP; ++p) mx = fmaxf(mx, fmaxf(s[p][r][e], s[p][r][e + 2]));
+                        for (int p = 0; p < GP; ++p)
+#pragma unroll
+                            for (int h = 0; h < 4; h += 2)
+                                if (admits(p, r, e + h)) mx = fmaxf(mx, s[p][r][e + h] * sc);
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        if (mx > m[r][e] + RESCALE_LOG2) {
+                        if (mx > m[r][e]) {  // (also where there was none)
                             const float f = ex2_approx(m[r][e] - mx);
-                            m[r][e] = mx;
+                            m[r][e] = ref[r][e] = mx;
                             l[r][e] *= f;
 #pragma unroll
                             for (int i = 0; i < C::MB; ++i) {
@@ -186,20 +284,56 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                             }
                         }
                     }
+                exps();
             }
 #pragma unroll
-            for (int p = 0; p < GP; ++p)
+            for (int r = 0; r < R8; ++r) {
+                l[r][0] += sum[r][0];
+                l[r][1] += sum[r][1];
 #pragma unroll
-                for (int r = 0; r < R8; ++r) {
-                    float q[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) q[e] = ex2_approx(s[p][r][e] - (m[r][e & 1] == -INFINITY ? 0.f : m[r][e & 1]));
-                    l[r][0] += q[0] + q[2];
-                    l[r][1] += q[1] + q[3];
-                    pf[p][r][0] = movmatrix(pack_bf16x2(q[0], q[1]));
-                    pf[p][r][1] = movmatrix(pack_bf16x2(q[2], q[3]));
+                for (int p = 0; p < GP; ++p) {
+                    pf[p][r][0] = movmatrix(pack_bf16x2(q[p][r][0], q[p][r][1]));
+                    pf[p][r][1] = movmatrix(pack_bf16x2(q[p][r][2], q[p][r][3]));
                 }
+            }
         };
+
+        if (tree) {
+            float s[1][R8][4];
+#pragma unroll
+            for (int r = 0; r < R8; ++r)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[0][r][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < C::RUN / 8; ++i) {
+                const uint32_t lo[4] = {kx[0][i].x, kx[0][i].y, kx[0][i].z, kx[0][i].w};
+                const uint32_t hi[4] = {kx[1][i].x, kx[1][i].y, kx[1][i].z, kx[1][i].w};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t af[4] = {lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1]};
+#pragma unroll
+                    for (int r = 0; r < R8; ++r) mma_bf16_16816(s[0][r], af, qf[r][4 * i + 2 * h], qf[r][4 * i + 2 * h + 1]);
+                }
+            }
+            uint32_t pf[1][R8][2];
+            const int n0 = 16 * warp + k_tok;
+            softmax(s, true, false, [&](int, int r, int e) {
+                const int gr = row0 + 8 * r + 2 * c + (e & 1);
+                return gr < a.rows && ((mask.anc[gr / G] >> (n0 + (e & 2 ? 8 : 0))) & 1ull);
+            }, pf);
+#pragma unroll
+            for (int i = 0; i < C::VRUN / 8; ++i) {
+                const uint32_t x[4][4] = {{vx[0][i].x, vx[0][i].y, vx[0][i].z, vx[0][i].w}, {vx[1][i].x, vx[1][i].y, vx[1][i].z, vx[1][i].w},
+                                          {vx[2][i].x, vx[2][i].y, vx[2][i].z, vx[2][i].w}, {vx[3][i].x, vx[3][i].y, vx[3][i].z, vx[3][i].w}};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t af[4] = {__byte_perm(x[0][j], x[1][j], 0x5410), __byte_perm(x[0][j], x[1][j], 0x7632),
+                                            __byte_perm(x[2][j], x[3][j], 0x5410), __byte_perm(x[2][j], x[3][j], 0x7632)};
+#pragma unroll
+                    for (int r = 0; r < R8; ++r) mma_bf16_16816(o[r][4 * i + j], af, pf[0][r][0], pf[0][r][1]);
+                }
+            }
+        }
 
         bool ok = true;
         for (int i = 0; i < n_i; ++i) {
@@ -208,7 +342,6 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const unsigned char *tile = mine + st * C::BYTES;
-            const uint32_t keep = (absent >> st) & 1u ? 0u : 0xffffffffu;
             // ---- S^T = K Q^T
             float s[2][R8][4];
 #pragma unroll
@@ -230,7 +363,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                         kw[h][0] = x.x, kw[h][1] = x.y;
                     }
                     const uint32_t sb = tile[C::CODES + (t0 + 8 * h) * Kv4<D>::SROW + (D == 128 ? c : c >> 1)];
-                    s2[h] = kv4_scale_pair(sb, sb) & keep;
+                    s2[h] = kv4_scale_twice(sb);
                     o2[h] = kv4_offset(s2[h]);
                 }
 #pragma unroll
@@ -249,7 +382,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             // ---- softmax
             uint32_t pf[2][R8][2];
             const int left = L - (first + i * SPECROLL_PAGE_TOKENS) - k_tok;  // > 0: token k_tok is in the sequence
-            softmax(s, [&](int p, int, int e) { return left > 16 * p + (e & 2 ? 8 : 0); }, pf);
+            softmax(s, i == 0, left + k_tok >= SLICE, [&](int p, int, int e) { return left > 16 * p + (e & 2 ? 8 : 0); }, pf);
             // ---- O^T += V^T P^T
             const unsigned char *vt = tile + C::HALF;
 #pragma unroll
@@ -267,7 +400,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     }
                     sb[q] = vt[C::CODES + tok * Kv4<D>::SROW + (g * C::VRUN) / 32];
                 }
-                const uint32_t s0 = kv4_scale_pair(sb[0], sb[1]) & keep, s1 = kv4_scale_pair(sb[2], sb[3]) & keep;
+                const uint32_t s0 = kv4_scale_pair(sb[0], sb[1]), s1 = kv4_scale_pair(sb[2], sb[3]);
                 const uint32_t f0 = kv4_offset(s0), f1 = kv4_offset(s1);
 #pragma unroll
                 for (int j = 0; j < C::VRUN / 8; ++j) {
@@ -289,61 +422,6 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             if (i + STAGES < n_i) {
                 load(i + STAGES, next_page);
                 next_page = i + STAGES + 1 < n_i ? __ldg(pt + i + STAGES + 1) : 0;
-            }
-        }
-        if (ok && has_tree && 16 * warp < N) {
-            // ---- the tree's rows, bf16 from global memory, sixteen nodes a warp
-            float s[1][R8][4];
-#pragma unroll
-            for (int r = 0; r < R8; ++r)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[0][r][e] = 0.f;
-            const size_t rows_of_b = (size_t)b * N;
-            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-            uint4 kx[2][C::RUN / 8];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int n = 16 * warp + k_tok + 8 * h;
-                const uint4 *src = reinterpret_cast<const uint4 *>(a.Kt + ((rows_of_b + n) * a.Hkv + hkv) * D + C::RUN * c);
-#pragma unroll
-                for (int i = 0; i < C::RUN / 8; ++i) kx[h][i] = n < N ? __ldg(src + i) : zero;
-            }
-#pragma unroll
-            for (int i = 0; i < C::RUN / 8; ++i) {
-                const uint32_t lo[4] = {kx[0][i].x, kx[0][i].y, kx[0][i].z, kx[0][i].w};
-                const uint32_t hi[4] = {kx[1][i].x, kx[1][i].y, kx[1][i].z, kx[1][i].w};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t af[4] = {lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1]};
-#pragma unroll
-                    for (int r = 0; r < R8; ++r) mma_bf16_16816(s[0][r], af, qf[r][4 * i + 2 * h], qf[r][4 * i + 2 * h + 1]);
-                }
-            }
-            uint32_t pf[1][R8][2];
-            const int n0 = 16 * warp + k_tok;
-            softmax(s, [&](int, int r, int e) {
-                const int gr = row0 + 8 * r + 2 * c + (e & 1);
-                return gr < a.rows && ((mask.anc[gr / G] >> (n0 + (e & 2 ? 8 : 0))) & 1ull);
-            }, pf);
-            uint4 vx[4][C::VRUN / 8];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = 16 * warp + ((q & 1) ? v_b : v_a) + 8 * (q >> 1);
-                const uint4 *src = reinterpret_cast<const uint4 *>(a.Vt + ((rows_of_b + n) * a.Hkv + hkv) * D + C::VRUN * g);
-#pragma unroll
-                for (int i = 0; i < C::VRUN / 8; ++i) vx[q][i] = n < N ? __ldg(src + i) : zero;
-            }
-#pragma unroll
-            for (int i = 0; i < C::VRUN / 8; ++i) {
-                const uint32_t x[4][4] = {{vx[0][i].x, vx[0][i].y, vx[0][i].z, vx[0][i].w}, {vx[1][i].x, vx[1][i].y, vx[1][i].z, vx[1][i].w},
-                                          {vx[2][i].x, vx[2][i].y, vx[2][i].z, vx[2][i].w}, {vx[3][i].x, vx[3][i].y, vx[3][i].z, vx[3][i].w}};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t af[4] = {__byte_perm(x[0][j], x[1][j], 0x5410), __byte_perm(x[0][j], x[1][j], 0x7632),
-                                            __byte_perm(x[2][j], x[3][j], 0x5410), __byte_perm(x[2][j], x[3][j], 0x7632)};
-#pragma unroll
-                    for (int r = 0; r < R8; ++r) mma_bf16_16816(o[r][4 * i + j], af, pf[0][r][0], pf[0][r][1]);
-                }
             }
         }
 #pragma unroll
@@ -433,7 +511,8 @@ static int launch_kv4(const AttnArgs &a, const TopoMask &mask, int32_t *status, 
 
 // Sums the chunks of every split sequence.  grid = (B, Hkv, 4): a block has a quarter of D of all rows of one (sequence, KV head), 4 D floats
 // of which a thread takes four, and as many parts of the chunks as 256 threads have room for; a part's chunks are taken eight at a
-// time with all their loads in flight.  Launched as a programmatic dependent of the attention kernel; the plan is complete when it starts.
+// time with all their loads in flight.  Launched as a programmatic dependent of the attention kernel, which
+// lets it start only behind its own wait: the lengths can be read ahead of the wait for the partials.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     constexpr int COLS = D / 16, ITEMS = ROWS * COLS, PARTS = 256 / ITEMS, STEP = 8;
@@ -442,9 +521,12 @@ __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     __shared__ float4 sh_acc[256];
     pdl_launch_dependents();
     const int b = blockIdx.x, hkv = blockIdx.y, part = threadIdx.x / ITEMS, row = threadIdx.x % ROWS, d4 = blockIdx.z * COLS + threadIdx.x % ITEMS / ROWS;
-    const int item0 = __ldcg(a.item_start + b), n_splits = __ldcg(a.item_start + b + 1) - item0;
+    const int len = max(__ldg(a.kv_len + b), 0);
+    const int n_splits = ((len + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS + a.chunk_tiles - 1) / a.chunk_tiles;
     if (n_splits < 2) return;
     pdl_wait();
+    const int item0 = __ldcg(a.item_start + b);
+    if (item0 < 0 || item0 + n_splits > a.items) return;  // (lengths that are not the host's)
     for (int rb = 0; rb < a.n_rb; ++rb) {
         const int gr = rb * ROWS + row;
         const size_t unit = (size_t)item0 * a.Hkv + hkv;

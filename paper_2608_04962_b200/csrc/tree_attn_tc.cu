@@ -676,7 +676,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 for (int i = 0; i < 4; ++i) dst[i] = stage_addr(st) + off[i];
 #pragma unroll
                 for (int it = 0; it < STEPS; ++it) {
-                    const uint32_t s2 = kv4_scale_pair(sb[it], sb[it]) & keep, o2 = kv4_offset(s2);
+                    const uint32_t s2 = kv4_scale_twice(sb[it]) & keep, o2 = kv4_offset(s2);
                     const uint32_t ww[4] = {w[it].x, w[it].y, w[it].z, w[it].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
