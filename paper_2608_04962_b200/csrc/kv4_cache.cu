@@ -5,6 +5,8 @@
 // A thread has eight elements (16 bytes of bf16, one 32-bit word of codes), four threads a block, so that both sides are
 // contiguous over a warp.  The arithmetic is kept to about four instructions an element, because the writer is otherwise
 // bound by it: a multiple of the reciprocal is added to a constant whose last four bits then are the code.
+#include <algorithm>
+
 #include "kv4.cuh"
 
 namespace specroll {
@@ -69,59 +71,99 @@ __device__ __forceinline__ void kv4_put(uint8_t *tile, int row, int at, uint32_t
     if ((at & 3) == 0) tile[Kv4<D>::CODES + row * Kv4<D>::SROW + (at >> 2)] = (uint8_t)scale;
 }
 
-constexpr int KV4_THREADS = 256;
+constexpr int KV4_THREADS = 256, KV4_EACH = 4;  // words of 16 bytes of bf16 that a thread takes side by side
 
-// Thread i has word i mod D/8 of row i / (D/8); rows are (token, K or V, head), so that a warp reads contiguous memory.
+// What the two kernels by slot share out: lines (a token's K or V of all heads: Hkv D / 8 words), `lines` to a block, so that a block has
+// about KV4_THREADS x KV4_EACH words; a warp reads and writes contiguous memory on the bf16 side.
+struct Kv4Lines {
+    const long long *slots;
+    long long n_lines, n_slots;  // 2 T; slots of the pool
+    int32_t lines, words, Hkv;   // lines of a block, words of a line
+    uint32_t by_words;           // floor(2^32 / words) + 1: a block's word number over `words` by multiplication
+};
+
+struct Kv4Word {
+    long long tok, slot;
+    int v, word;  // K or V; word of the line
+    bool in;
+};
+__device__ __forceinline__ Kv4Word kv4_word_of(const Kv4Lines &a, uint32_t i) {
+    const uint32_t l = __umulhi(i, a.by_words);
+    const long long line = (long long)blockIdx.x * a.lines + l;
+    Kv4Word w;
+    w.in = l < (uint32_t)a.lines && line < a.n_lines;
+    w.tok = line >> 1;
+    w.v = (int)(line & 1);
+    w.word = (int)(i - l * a.words);
+    w.slot = w.in ? __ldg(a.slots + w.tok) : -1;
+    return w;
+}
+// Tile of a word, and its token's row there.
+template <int D>
+__device__ __forceinline__ long long kv4_tile_of(const Kv4Lines &a, const Kv4Word &w) {
+    return (((w.slot >> 7) * a.Hkv + w.word / (D / 8)) * 2 + w.v) * (long long)Kv4<D>::TILE;
+}
+static_assert(SPECROLL_PAGE_TOKENS == 128, "slot >> 7");
+
 template <int D>
 __global__ void __launch_bounds__(KV4_THREADS)
-kv4_store_kernel(const uint4 *__restrict__ K, const uint4 *__restrict__ V, const long long *__restrict__ slots, long long n_words, int Hkv,
-                 uint8_t *__restrict__ pool, long long n_slots, int32_t *__restrict__ status) {
+kv4_store_kernel(const uint4 *__restrict__ K, const uint4 *__restrict__ V, const Kv4Lines a, uint8_t *__restrict__ pool,
+                 int32_t *__restrict__ status) {
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int W = D / 8;
-    const long long i = (long long)blockIdx.x * KV4_THREADS + threadIdx.x;
-    const bool in = i < n_words;  // (whole blocks of 32 elements at a time: n_words is a multiple of W)
-    const int at = (int)(i % W), heads = Hkv * W;
-    const long long line = i / heads;  // token and K or V
-    const int head = (int)((i - line * heads) / W), v = (int)(line & 1);
-    const long long tok = line >> 1;
-    const long long slot = in ? __ldg(slots + tok) : -1;
-    const bool ok = slot >= 0 && slot < n_slots;
-    const uint4 x = ok ? __ldg((v ? V : K) + tok * heads + head * W + at) : make_uint4(0u, 0u, 0u, 0u);
-    uint32_t scale;
-    const uint32_t codes = kv4_encode(x, scale);
-    if (ok) {
-        uint8_t *tile = pool + ((slot / SPECROLL_PAGE_TOKENS * Hkv + head) * 2 + v) * (long long)Kv4<D>::TILE;
-        kv4_put<D>(tile, (int)(slot % SPECROLL_PAGE_TOKENS), at, codes, scale);
-    } else if (in && slot >= n_slots && status && at == 0 && head == 0) {
-        atomicExch(status, SPECROLL_ELIMIT);
+    for (uint32_t i0 = threadIdx.x; i0 - threadIdx.x < (uint32_t)(a.lines * a.words); i0 += KV4_THREADS * KV4_EACH) {
+        Kv4Word w[KV4_EACH];
+        uint4 x[KV4_EACH];
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) w[q] = kv4_word_of(a, i0 + q * KV4_THREADS);
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) {
+            const bool ok = w[q].slot >= 0 && w[q].slot < a.n_slots;
+            x[q] = ok ? ld_nc_v4((w[q].v ? V : K) + w[q].tok * a.words + w[q].word) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) {
+            uint32_t scale;
+            const uint32_t codes = kv4_encode(x[q], scale);  // (four threads a block of 32, all in it together)
+            if (w[q].slot >= 0 && w[q].slot < a.n_slots)
+                kv4_put<D>(pool + kv4_tile_of<D>(a, w[q]), (int)(w[q].slot & 127), w[q].word % (D / 8), codes, scale);
+            else if (w[q].in && w[q].slot >= 0 && status && w[q].word == 0)
+                atomicExch(status, SPECROLL_ELIMIT);
+        }
     }
 }
 
 template <int D>
 __global__ void __launch_bounds__(KV4_THREADS)
-kv4_load_kernel(const uint8_t *__restrict__ pool, const long long *__restrict__ slots, long long n_words, int Hkv, long long n_slots,
-                uint4 *__restrict__ K, uint4 *__restrict__ V, int32_t *__restrict__ status) {
+kv4_load_kernel(const uint8_t *__restrict__ pool, const Kv4Lines a, uint4 *__restrict__ K, uint4 *__restrict__ V, int32_t *__restrict__ status) {
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int W = D / 8;
-    const long long i = (long long)blockIdx.x * KV4_THREADS + threadIdx.x;
-    if (i >= n_words) return;
-    const int at = (int)(i % W), heads = Hkv * W;
-    const long long line = i / heads;
-    const int head = (int)((i - line * heads) / W), v = (int)(line & 1);
-    const long long tok = line >> 1, slot = __ldg(slots + tok);
-    uint32_t r[4] = {0u, 0u, 0u, 0u};
-    if (slot >= 0 && slot < n_slots) {
-        const uint8_t *tile = pool + ((slot / SPECROLL_PAGE_TOKENS * Hkv + head) * 2 + v) * (long long)Kv4<D>::TILE;
-        const int row = (int)(slot % SPECROLL_PAGE_TOKENS);
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(tile + row * Kv4<D>::ROW) + at);
-        const uint32_t s = kv4_scale_bits(__ldg(tile + Kv4<D>::CODES + row * Kv4<D>::SROW + (at >> 2))) * 0x10001u;
-        kv4_word(w, s, kv4_offset(s), r);
-    } else if (slot >= n_slots && status && at == 0 && head == 0) {
-        atomicExch(status, SPECROLL_ELIMIT);
+    for (uint32_t i0 = threadIdx.x; i0 - threadIdx.x < (uint32_t)(a.lines * a.words); i0 += KV4_THREADS * KV4_EACH) {
+        Kv4Word w[KV4_EACH];
+        uint32_t codes[KV4_EACH], scale[KV4_EACH];
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) w[q] = kv4_word_of(a, i0 + q * KV4_THREADS);
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) {
+            codes[q] = 0x88888888u;  // (zeros)
+            scale[q] = 0u;
+            if (w[q].slot >= 0 && w[q].slot < a.n_slots) {
+                const uint8_t *tile = pool + kv4_tile_of<D>(a, w[q]);
+                const int row = (int)(w[q].slot & 127), at = w[q].word % (D / 8);
+                codes[q] = __ldg(reinterpret_cast<const uint32_t *>(tile + row * Kv4<D>::ROW) + at);
+                scale[q] = __ldg(tile + Kv4<D>::CODES + row * Kv4<D>::SROW + (at >> 2));
+            } else if (w[q].in && w[q].slot >= 0 && status && w[q].word == 0) {
+                atomicExch(status, SPECROLL_ELIMIT);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) {
+            uint32_t r[4];
+            const uint32_t s = kv4_scale_twice(scale[q]);
+            kv4_word(codes[q], s, kv4_offset(s), r);
+            if (w[q].in) __stcs((w[q].v ? V : K) + w[q].tok * a.words + w[q].word, make_uint4(r[0], r[1], r[2], r[3]));
+        }
     }
-    (v ? V : K)[tok * heads + head * W + at] = make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 constexpr int KV4_COMMIT_LAYERS = 64;  // layers one launch can serve (their pointers travel as kernel arguments)
@@ -131,42 +173,70 @@ struct Kv4Layers {
     uint8_t *pool[KV4_COMMIT_LAYERS];
 };
 
-// grid = (B, K + 1, layers): block (b, i, l) writes tree row path_node[b, i] of layer l at cache position kv_len[b] + i, as
-// commit_path_kernel does for a bf16 cache.
+// grid = (B, groups of `each` layers): the committed rows of sequence b go to cache positions kv_len[b] + i of those layers' pools, as
+// commit_path_kernel has it for a bf16 cache.  The first warp finds the rows' places, once for K, V and all layers of the group (a block
+// for every row and layer spent its time on that chain of loads: 40 us instead of 13 for 256 sequences, 28 layers of two heads);
+// a thread then takes four words at a time.
 template <int D>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(KV4_THREADS)
 kv4_commit_kernel(const __grid_constant__ Kv4Layers lay, const int32_t *__restrict__ path_node, const int32_t *__restrict__ n_acc,
                   long long n_pages, const int32_t *__restrict__ page_table, const int32_t *__restrict__ page_indptr,
-                  const int32_t *__restrict__ kv_len, int N, int K, int Hkv, int32_t *__restrict__ status, int32_t *__restrict__ kv_len_out) {
+                  const int32_t *__restrict__ kv_len, int N, int K, int Hkv, int n_layers, int each, int32_t *__restrict__ status,
+                  int32_t *__restrict__ kv_len_out) {
+    constexpr int W = D / 8;
+    __shared__ long long sh_src[SPECROLL_MAX_HEADS + 1], sh_dst[SPECROLL_MAX_HEADS + 1];  // first word of the tree row; slot
+    __shared__ int sh_rows;
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int W = D / 8;
-    const int b = blockIdx.x, i = blockIdx.y;
-    const int na = n_acc[b], len = kv_len[b];
-    if (kv_len_out && i == 0 && blockIdx.z == 0 && threadIdx.x == 0) kv_len_out[b] = len + ((na < 0 || na > K) ? 0 : na + 1);
-    if (i > na || na < 0 || na > K) return;
-    const int node = path_node[(size_t)b * (K + 1) + i];
-    const long long pos = (long long)len + i, slot = pos / SPECROLL_PAGE_TOKENS;
-    const int first = page_indptr[b], own = page_indptr[b + 1] - first;
-    int page = -1;
-    if (node >= 0 && node < N && len >= 0 && slot < own) page = page_table[first + slot];
-    if (page < 0 || page >= n_pages) {
+    const int b = blockIdx.x;
+    if (threadIdx.x < 32) {
+        const int i = threadIdx.x, na = n_acc[b], len = kv_len[b], first = page_indptr[b], own = page_indptr[b + 1] - first;
+        const bool committed = na >= 0 && na <= K;
+        const bool mine = committed && i <= na;
+        const int node = mine ? path_node[(size_t)b * (K + 1) + i] : -1;
+        const long long pos = (long long)len + i, at = pos / SPECROLL_PAGE_TOKENS;
+        int page = -1;
+        if (node >= 0 && node < N && len >= 0 && at < own) page = page_table[first + at];
+        const bool ok = page >= 0 && page < n_pages;
         // no room (or a bad table): nothing is written for this token, and the caller is told
-        if (threadIdx.x == 0 && status) atomicExch(status, SPECROLL_ELIMIT);
-        return;
+        if (mine && !ok && status && blockIdx.y == 0) atomicExch(status, SPECROLL_ELIMIT);
+        const uint32_t have = __ballot_sync(0xffffffffu, ok);
+        if (ok) {
+            const int r = __popc(have & ((1u << i) - 1u));
+            sh_src[r] = ((long long)b * N + node) * Hkv * W;
+            sh_dst[r] = (long long)page * SPECROLL_PAGE_TOKENS + pos % SPECROLL_PAGE_TOKENS;
+        }
+        if (i == 0) {
+            sh_rows = __popc(have);
+            if (kv_len_out && blockIdx.y == 0) kv_len_out[b] = len + (committed ? na + 1 : 0);
+        }
     }
-    const int heads = Hkv * W, row = (int)(pos % SPECROLL_PAGE_TOKENS);
-    const uint4 *const Kt = lay.Kt[blockIdx.z], *const Vt = lay.Vt[blockIdx.z];
-    uint8_t *const tiles = lay.pool[blockIdx.z] + (size_t)page * Hkv * 2 * Kv4<D>::TILE;
-    const size_t src = ((size_t)b * N + node) * heads;
-    for (int w0 = 0; w0 < 2 * heads; w0 += 128) {  // (whole warps: the four threads of a block meet in the encoder)
-        const int w = w0 + (int)threadIdx.x;
-        const bool in = w < 2 * heads;
-        const int v = w >= heads, word = v ? w - heads : w;
-        const uint4 x = in ? __ldg((v ? Vt : Kt) + src + word) : make_uint4(0u, 0u, 0u, 0u);
-        uint32_t scale;
-        const uint32_t codes = kv4_encode(x, scale);
-        if (in) kv4_put<D>(tiles + (size_t)(word / W * 2 + v) * Kv4<D>::TILE, row, word % W, codes, scale);
+    __syncthreads();
+    // words in the order (layer, row, K or V, head, word of the head)
+    const int heads = Hkv * W, l0 = blockIdx.y * each, per_layer = sh_rows * 2 * heads, total = per_layer * min(each, n_layers - l0);
+    for (int i0 = threadIdx.x; i0 - (int)threadIdx.x < total; i0 += KV4_THREADS * KV4_EACH) {
+        uint4 x[KV4_EACH];
+        uint8_t *tile[KV4_EACH];
+        int row[KV4_EACH], at[KV4_EACH];
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) {
+            const int i = i0 + q * KV4_THREADS;
+            tile[q] = nullptr;
+            x[q] = make_uint4(0u, 0u, 0u, 0u);
+            if (i >= total) continue;
+            const int l = i / per_layer, j = i - l * per_layer, r = j / (2 * heads), w = j - r * 2 * heads, v = w >= heads, word = v ? w - heads : w;
+            const long long slot = sh_dst[r];
+            x[q] = ld_nc_v4((v ? lay.Vt[l0 + l] : lay.Kt[l0 + l]) + sh_src[r] + word);
+            tile[q] = lay.pool[l0 + l] + ((slot / SPECROLL_PAGE_TOKENS * Hkv + word / W) * 2 + v) * (long long)Kv4<D>::TILE;
+            row[q] = (int)(slot % SPECROLL_PAGE_TOKENS);
+            at[q] = word % W;
+        }
+#pragma unroll
+        for (int q = 0; q < KV4_EACH; ++q) {
+            uint32_t scale;
+            const uint32_t codes = kv4_encode(x[q], scale);
+            if (tile[q]) kv4_put<D>(tile[q], row[q], at[q], codes, scale);
+        }
     }
 }
 
@@ -187,39 +257,47 @@ extern "C" size_t specroll_kv4_tile_bytes(int32_t D) {
     return D == 64 ? Kv4<64>::TILE : D == 128 ? Kv4<128>::TILE : 0;
 }
 
-// What the two calls by slot share.  *n_words: 16-byte words of bf16 over both K and V.
-static int by_slot_check(int64_t T, int32_t Hkv, int32_t D, const void *K, const void *V, const int64_t *slots, const void *pool,
-                         int64_t n_pages, long long *n_words) {
-    if (T < 0 || T > (1LL << 31) || Hkv < 1 || Hkv > 4096 || (D != 64 && D != 128) || n_pages < 0 || n_pages > (1LL << 24)) return SPECROLL_EINVAL;
-    *n_words = 2LL * T * Hkv * (D / 8);
-    if ((*n_words + KV4_THREADS - 1) / KV4_THREADS > 0x7fffffffLL) return SPECROLL_EINVAL;
+// What the two calls by slot share: the checks, and how the lines are shared out (*blocks = 0: nothing to do).
+static int by_slot(int64_t T, int32_t Hkv, int32_t D, const void *K, const void *V, const int64_t *slots, const void *pool, int64_t n_pages,
+                   Kv4Lines *a, unsigned *blocks) {
+    *blocks = 0;
+    if (T < 0 || T > (1LL << 30) || Hkv < 1 || Hkv > 4096 || (D != 64 && D != 128) || n_pages < 0 || n_pages > (1LL << 24)) return SPECROLL_EINVAL;
     if (T == 0) return SPECROLL_OK;  // (no tokens have empty arrays: their pointers may be NULL)
     if (!K || !V || !slots || (n_pages > 0 && !pool)) return SPECROLL_EINVAL;
     if (!aligned16(K) || !aligned16(V) || !aligned16(pool)) return SPECROLL_EALIGN;
+    const int words = Hkv * (D / 8), most = KV4_THREADS * KV4_EACH;
+    a->slots = reinterpret_cast<const long long *>(slots);
+    a->n_lines = 2 * T;
+    a->n_slots = (long long)n_pages * SPECROLL_PAGE_TOKENS;
+    a->words = words;
+    a->lines = words < most ? most / words : 1;
+    a->Hkv = Hkv;
+    a->by_words = (uint32_t)((1ULL << 32) / (unsigned)words + 1);
+    *blocks = (unsigned)((a->n_lines + a->lines - 1) / a->lines);
     return SPECROLL_OK;
 }
 
 extern "C" int specroll_kv4_store(int64_t T, int32_t Hkv, int32_t D, const void *K, const void *V, const int64_t *slot_map, void *pool,
                                   int64_t n_pages, int32_t *status, void *cuda_stream) {
-    long long n = 0;
-    const int rc = by_slot_check(T, Hkv, D, K, V, slot_map, pool, n_pages, &n);
-    if (rc != SPECROLL_OK || T == 0) return rc;
-    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_store_kernel<128> : kv4_store_kernel<64>, dim3((unsigned)((n + KV4_THREADS - 1) / KV4_THREADS)),
-                                 dim3(KV4_THREADS), 0, static_cast<cudaStream_t>(cuda_stream), static_cast<const uint4 *>(K),
-                                 static_cast<const uint4 *>(V), reinterpret_cast<const long long *>(slot_map), n, Hkv, static_cast<uint8_t *>(pool),
-                                 (long long)n_pages * SPECROLL_PAGE_TOKENS, status));
+    Kv4Lines a;
+    unsigned blocks = 0;
+    const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &blocks);
+    if (rc != SPECROLL_OK || !blocks) return rc;
+    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_store_kernel<128> : kv4_store_kernel<64>, dim3(blocks), dim3(KV4_THREADS), 0,
+                                 static_cast<cudaStream_t>(cuda_stream), static_cast<const uint4 *>(K), static_cast<const uint4 *>(V), a,
+                                 static_cast<uint8_t *>(pool), status));
     return SPECROLL_OK;
 }
 
 extern "C" int specroll_kv4_load(int64_t T, int32_t Hkv, int32_t D, const void *pool, int64_t n_pages, const int64_t *slot_map, void *K,
                                  void *V, int32_t *status, void *cuda_stream) {
-    long long n = 0;
-    const int rc = by_slot_check(T, Hkv, D, K, V, slot_map, pool, n_pages, &n);
-    if (rc != SPECROLL_OK || T == 0) return rc;
-    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_load_kernel<128> : kv4_load_kernel<64>, dim3((unsigned)((n + KV4_THREADS - 1) / KV4_THREADS)),
-                                 dim3(KV4_THREADS), 0, static_cast<cudaStream_t>(cuda_stream), static_cast<const uint8_t *>(pool),
-                                 reinterpret_cast<const long long *>(slot_map), n, Hkv, (long long)n_pages * SPECROLL_PAGE_TOKENS,
-                                 static_cast<uint4 *>(K), static_cast<uint4 *>(V), status));
+    Kv4Lines a;
+    unsigned blocks = 0;
+    const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &blocks);
+    if (rc != SPECROLL_OK || !blocks) return rc;
+    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_load_kernel<128> : kv4_load_kernel<64>, dim3(blocks), dim3(KV4_THREADS), 0,
+                                 static_cast<cudaStream_t>(cuda_stream), static_cast<const uint8_t *>(pool), a, static_cast<uint4 *>(K),
+                                 static_cast<uint4 *>(V), status));
     return SPECROLL_OK;
 }
 
@@ -237,6 +315,9 @@ extern "C" int specroll_commit_path_kv4_layers(int32_t B, int32_t N, int32_t K, 
         if (!aligned16(Kt[l]) || !aligned16(Vt[l]) || !aligned16(pool[l])) return SPECROLL_EALIGN;
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    int n_sm = 0;
+    const int rc = device_setup(nullptr, 0, &n_sm);
+    if (rc != SPECROLL_OK) return rc;
     const bool apart = kv_len_out && (kv_len_out >= kv_len + B || kv_len_out + B <= kv_len);
     for (int l0 = 0; l0 < n_layers; l0 += KV4_COMMIT_LAYERS) {
         const int nl = n_layers - l0 < KV4_COMMIT_LAYERS ? n_layers - l0 : KV4_COMMIT_LAYERS;
@@ -246,9 +327,11 @@ extern "C" int specroll_commit_path_kv4_layers(int32_t B, int32_t N, int32_t K, 
             lay.Vt[l] = static_cast<const uint4 *>(Vt[l0 + l]);
             lay.pool[l] = static_cast<uint8_t *>(pool[l0 + l]);
         }
+        // layers to a block: as many as leave four blocks to every SM
+        const int each = (int)std::min<long long>(std::max<long long>((long long)B * nl / (4LL * n_sm), 1), 8);
         SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_commit_kernel<128> : kv4_commit_kernel<64>,
-                                     dim3((unsigned)B, (unsigned)(K + 1), (unsigned)nl), dim3(128), 0, st, lay, path_node, n_acc,
-                                     (long long)n_pages, page_table, page_indptr, kv_len, N, K, Hkv, status,
+                                     dim3((unsigned)B, (unsigned)((nl + each - 1) / each)), dim3(KV4_THREADS), 0, st, lay, path_node, n_acc,
+                                     (long long)n_pages, page_table, page_indptr, kv_len, N, K, Hkv, nl, each, status,
                                      apart && l0 == 0 ? kv_len_out : nullptr));
     }
     // in place: after the copies in stream order

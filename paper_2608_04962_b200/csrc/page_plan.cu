@@ -12,7 +12,7 @@ namespace specroll {
 
 constexpr int PLAN_MAX_B = 4096, PLAN_THREADS = 512;
 constexpr int PLAN_PER = 4;  // neighbouring slots a thread writes at a time (two 16-byte stores)
-constexpr long long PLAN_SAT = 0x7fffffffLL;
+constexpr uint32_t PLAN_SAT = 0x7fffffffu;
 
 struct PagePlanArgs {
     const int32_t *kv_len, *add, *table, *indptr, *free_list, *n_free;
@@ -33,82 +33,88 @@ __device__ __forceinline__ int plan_seq_of(const int32_t *sum, int B, int at) {
     return lo;
 }
 
+// Sums stop at 2^31 - 1: what is beyond is beyond every capacity too, and reported.
+__device__ __forceinline__ uint32_t plan_add(uint32_t x, uint32_t y) { return min(x + y, PLAN_SAT); }
+
 __global__ void __launch_bounds__(PLAN_THREADS)
 page_plan_kernel(const PagePlanArgs a) {
-    extern __shared__ int32_t sums[];  // [4][B + 1]
-    __shared__ long long warp_tot[4][PLAN_THREADS / 32];
+    extern __shared__ int32_t sums[];  // [4][B + 1] running sums, then of every sequence its first old page's place, its old pages, its length
+    __shared__ uint32_t warp_tot[4][PLAN_THREADS / 32];
     pdl_wait();
     pdl_launch_dependents();
     const int B = a.B, t = threadIdx.x, lane = t & 31, warp = t >> 5;
     int32_t *const owns = sums, *const toks = sums + (B + 1), *const takes = toks + (B + 1), *const gives = takes + (B + 1);
-    const int nf = min(max(*a.n_free, 0), a.free_cap);
+    int32_t *const old_at = gives + (B + 1), *const hads = old_at + B, *const lens = hads + B;
+    const int nf_given = __ldg(a.n_free);
 
-    // ---- per sequence: pages it had, takes, owns afterwards, gives back, and its new tokens; then the running sums.  They are
-    // made in 64 bits and kept to 31: what is beyond is beyond every capacity too, and reported.
-    const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = t * per, b1 = min(B, b0 + per);
-    auto of_seq = [&](int b, long long (&v)[4]) {
-        const int add = a.add[b];
-        const long long len = max(a.kv_len[b], 0);
-        const int had = max(a.indptr[b + 1] - a.indptr[b], 0);
-        const long long need = (len + max(add, 0) + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS;
-        v[2] = add < 0 ? 0 : max(need - had, 0LL);
-        v[0] = add < 0 ? 0 : had + v[2];
-        v[1] = max(add, 0);
-        v[3] = add < 0 ? had : 0;
+    // ---- per sequence: pages it owns afterwards, new tokens, pages it takes, pages it gives back; then the running sums
+    const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(B, t * per), b1 = min(B, b0 + per);
+    auto of_seq = [&](int b, int add, uint32_t (&v)[4]) {
+        const uint32_t had = (uint32_t)hads[b], more = add < 0 ? 0u : (uint32_t)add;
+        const uint32_t need = ((uint32_t)lens[b] + more + (SPECROLL_PAGE_TOKENS - 1)) / SPECROLL_PAGE_TOKENS;  // (below 2^32: both are below 2^31)
+        v[1] = more;
+        v[2] = add < 0 || need < had ? 0u : need - had;
+        v[0] = add < 0 ? 0u : had + v[2];
+        v[3] = add < 0 ? had : 0u;
     };
-    long long run[4] = {0, 0, 0, 0}, tot[4];
+    uint32_t run[4] = {0u, 0u, 0u, 0u}, tot[4], one[4];
     for (int b = b0; b < b1; ++b) {
-        long long v[4];
-        of_seq(b, v);
+        const int at = a.indptr[b], end = a.indptr[b + 1], add = a.add[b], len = a.kv_len[b];
+        old_at[b] = at;
+        hads[b] = max(end - at, 0);
+        lens[b] = max(len, 0);
+        of_seq(b, add, one);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) run[q] += v[q];
+        for (int q = 0; q < 4; ++q) run[q] = plan_add(run[q], one[q]);
     }
+    uint32_t before[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const long long mine = run[q];
+        uint32_t incl = run[q];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, run[q], o);
-            if (lane >= o) run[q] += x;
+            const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl = plan_add(incl, x);
         }
-        if (lane == 31) warp_tot[q][warp] = run[q];
-        run[q] -= mine;  // exclusive within the warp
+        if (lane == 31) warp_tot[q][warp] = incl;
+        before[q] = __shfl_up_sync(0xffffffffu, incl, 1);  // exclusive within the warp
+        if (lane == 0) before[q] = 0u;
     }
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        long long before = 0, all = 0;
+        uint32_t ahead = 0u, all = 0u;
 #pragma unroll
         for (int w = 0; w < PLAN_THREADS / 32; ++w) {
-            const long long x = warp_tot[q][w];
-            before += w < warp ? x : 0;
-            all += x;
+            const uint32_t x = warp_tot[q][w];
+            ahead = w < warp ? plan_add(ahead, x) : ahead;
+            all = plan_add(all, x);
         }
-        run[q] += before;
+        run[q] = plan_add(before[q], ahead);
         tot[q] = all;
     }
     for (int b = b0; b < b1; ++b) {
-        long long v[4];
-        of_seq(b, v);
+        if (per > 1) of_seq(b, a.add[b], one);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            sums[q * (B + 1) + b] = (int32_t)min(run[q], PLAN_SAT);
-            run[q] += v[q];
+            sums[q * (B + 1) + b] = (int32_t)run[q];
+            run[q] = plan_add(run[q], one[q]);
         }
     }
-    if (t < 4) sums[t * (B + 1) + B] = (int32_t)min(t == 0 ? tot[0] : t == 1 ? tot[1] : t == 2 ? tot[2] : tot[3], PLAN_SAT);
+    if (t < 4) sums[t * (B + 1) + B] = (int32_t)(t == 0 ? tot[0] : t == 1 ? tot[1] : t == 2 ? tot[2] : tot[3]);
     __syncthreads();
 
+    const int nf = min(max(nf_given, 0), a.free_cap);
     const long long left = max((long long)nf - tot[2], 0LL), free_after = left + tot[3];
     if (blockIdx.x == 0 && t == 0) {
         *a.n_free_out = (int32_t)min(free_after, (long long)a.free_cap);
-        if (a.status && (tot[2] > nf || tot[0] > a.table_cap || tot[1] > min(a.slot_cap, PLAN_SAT) || free_after > a.free_cap))
+        if (a.status && (tot[2] > (uint32_t)nf || tot[0] > (uint32_t)a.table_cap || tot[1] > min(a.slot_cap, (long long)PLAN_SAT - 1) || free_after > a.free_cap))
             atomicExch(a.status, SPECROLL_ELIMIT);
     }
 
     // the pages as they were, and those of the free list, by place; -1 where there is none
     auto old_page = [&](int b, int i) -> int {
-        const long long at = (long long)a.indptr[b] + i;
+        const long long at = (long long)old_at[b] + i;
         return at >= 0 && at < a.n_table ? __ldg(a.table + at) : -1;
     };
     auto new_page = [&](long long j) -> int { return j < nf ? __ldg(a.free_list + j) : -1; };
@@ -123,20 +129,20 @@ page_plan_kernel(const PagePlanArgs a) {
         int page = -1;
         if (i < tot[0]) {
             const int b = plan_seq_of(owns, B, (int)i);
-            page = page_of(b, (int)i - owns[b], max(a.indptr[b + 1] - a.indptr[b], 0));
+            page = page_of(b, (int)i - owns[b], hads[b]);
         }
         a.table_out[i] = page;
     }
     for (long long i = me; i < a.free_cap; i += stride) {
         int page = -1;
-        if (i < left) page = new_page(tot[2] + i);
+        if (i < left) page = new_page((long long)tot[2] + i);
         else if (i < free_after) {
             const int at = (int)(i - left), b = plan_seq_of(gives, B, at);
             page = old_page(b, at - gives[b]);
         }
         a.free_out[i] = page;
     }
-    const long long n_slots = min(a.slot_cap, PLAN_SAT);
+    const long long n_slots = min(a.slot_cap, (long long)PLAN_SAT);
     for (long long i0 = me * PLAN_PER; i0 < a.slot_cap; i0 += stride * PLAN_PER) {
         long long out[PLAN_PER];
         int b = -1, had = 0, end = -1, page = -1;
@@ -145,12 +151,12 @@ page_plan_kernel(const PagePlanArgs a) {
         for (int q = 0; q < PLAN_PER; ++q) {
             const long long i = i0 + q;
             out[q] = -1;
-            if (i >= min(tot[1], n_slots)) continue;
+            if (i >= min((long long)tot[1], n_slots)) continue;
             if (i >= end) {
                 b = plan_seq_of(toks, B, (int)i);
                 end = toks[b + 1];
-                had = max(a.indptr[b + 1] - a.indptr[b], 0);
-                first = (long long)max(a.kv_len[b], 0) - toks[b];
+                had = hads[b];
+                first = (long long)lens[b] - toks[b];
                 in_page = -1;
             }
             const long long pos = first + i, p = pos / SPECROLL_PAGE_TOKENS;
@@ -175,6 +181,8 @@ page_plan_kernel(const PagePlanArgs a) {
 
 using namespace specroll;
 
+static size_t plan_smem(int B) { return (size_t)(7 * B + 4) * sizeof(int32_t); }
+
 extern "C" int specroll_page_plan(int32_t B, const int32_t *kv_len, const int32_t *add, const int32_t *page_table, int32_t n_table,
                                   const int32_t *page_indptr, const int32_t *free_list, int32_t free_cap, const int32_t *n_free,
                                   int32_t table_cap, int64_t slot_cap, int32_t *page_table_out, int32_t *page_indptr_out,
@@ -191,9 +199,9 @@ extern "C" int specroll_page_plan(int32_t B, const int32_t *kv_len, const int32_
     if (meet(page_table, n_table, page_table_out, table_cap) || meet(free_list, free_cap, free_list_out, free_cap) || meet(n_free, 1, n_free_out, 1) ||
         meet(page_indptr, (long long)B + 1, page_indptr_out, (long long)B + 1))
         return SPECROLL_EINVAL;
-    const size_t smem = (size_t)4 * (B + 1) * sizeof(int32_t);
+    const size_t smem = plan_smem(B);
     int n_sm = 0;
-    const int rc = device_setup(reinterpret_cast<const void *>(page_plan_kernel), 4 * (PLAN_MAX_B + 1) * (int)sizeof(int32_t), &n_sm);
+    const int rc = device_setup(reinterpret_cast<const void *>(page_plan_kernel), (int)plan_smem(PLAN_MAX_B), &n_sm);
     if (rc != SPECROLL_OK) return rc;
     const PagePlanArgs a = {kv_len, add, page_table, page_indptr, free_list, n_free, page_table_out, page_indptr_out, tok_indptr,
                             free_list_out, n_free_out, status, reinterpret_cast<long long *>(slot_map), B, n_table, free_cap, table_cap,

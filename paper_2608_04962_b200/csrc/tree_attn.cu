@@ -91,8 +91,7 @@ attn_prep_kernel(const int32_t *__restrict__ kv_indptr, const int32_t *__restric
                  int32_t *__restrict__ item_start, int32_t *__restrict__ sorted_start,
                  int32_t *__restrict__ seq_at_rank, int32_t *__restrict__ unit_tab, int32_t *__restrict__ status,
                  int32_t *__restrict__ counters, int n_counters) {
-    __shared__ unsigned short sh_ns[PREP_MAX_B];  // chunk counts fit 16 bits (checked on the host)
-    __shared__ int sh_cost[PREP_MAX_B];
+    __shared__ __align__(16) int sh_key[PREP_MAX_B + 4];
     __shared__ int sh_tmp[PREP_MAX_B];
     __shared__ int warp_tot[33];
     const int t = threadIdx.x;
@@ -165,76 +164,86 @@ attn_prep_kernel(const int32_t *__restrict__ kv_indptr, const int32_t *__restric
         }
         return;
     }
-    for (int b = t; b < B; b += PREP_THREADS) {
-        int L = kv_len ? kv_len[b] : kv_indptr[b + 1] - kv_indptr[b];
+    // Thread i (of up to PREP_MAX_B, four passes) belongs to sequence i / per, so that few sequences are ranked and written by many
+    // threads; lengths and places are read once and stay in registers.
+    constexpr int PASSES = PREP_MAX_B / PREP_THREADS;
+    int per = 1;
+    while (per < 32 && 2 * per * B <= PREP_THREADS) per *= 2;
+    int L[PASSES], kv0[PASSES], ns[PASSES], first[PASSES], rank[PASSES];
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {
+        const int i = q * PREP_THREADS + t, b = i / per;
+        // contiguous cache: first token and length; paged cache: first slot of the page table and length
+        kv0[q] = b < B ? (kv_len ? page_indptr[b] : kv_indptr[b]) : 0;
+        L[q] = b < B ? (kv_len ? kv_len[b] : kv_indptr[b + 1] - kv0[q]) : 0;
 #ifdef SPECROLL_CHECK
-        if (L < 0) {  // the device copy of the lengths disagrees with any host copy the planner can have seen
+        if (L[q] < 0) {  // the device copy of the lengths disagrees with any host copy the planner can have seen
             SR_CHECK_FAIL(b);
-            L = 0;
+            L[q] = 0;
         }
 #endif
-        const int tiles = (L + tile_tokens - 1) / tile_tokens;
-        int ns = (tiles + chunk_tiles - 1) / chunk_tiles;
-        if (ns < 1) ns = 1;
-        sh_ns[b] = (unsigned short)ns;
-        sh_cost[b] = (tiles + ns - 1) / ns;  // tiles per chunk
-        sh_tmp[b] = ns;
     }
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {
+        const int i = q * PREP_THREADS + t, b = i / per;
+        const int tiles = (L[q] + tile_tokens - 1) / tile_tokens;
+        ns[q] = max(1, (tiles + chunk_tiles - 1) / chunk_tiles);
+        if (b < B && i % per == 0) {
+            sh_tmp[b] = ns[q];
+            // tiles per chunk, and before equal ones those of lower index: the larger key comes first
+            sh_key[b] = min((tiles + ns[q] - 1) / ns[q], (1 << 19) - 1) * PREP_MAX_B + (PREP_MAX_B - 1 - b);
+        }
+    }
+    if (t < 4) sh_key[B + t] = -1;
     __syncthreads();
     const int total = block_exclusive_scan(sh_tmp, B, warp_tot);
-    for (int b = t; b < B; b += PREP_THREADS) item_start[b] = sh_tmp[b];
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {
+        const int i = q * PREP_THREADS + t, b = i / per;
+        first[q] = b < B ? sh_tmp[b] : 0;
+        if (b < B && i % per == 0) item_start[b] = first[q];
+    }
     if (t == 0) item_start[B] = total;
     if (!sorted_start) return;
-    __syncthreads();
-    // rank by counting: position of b in the order (cost descending, index ascending); where there are fewer sequences than threads
-    // several threads count for one.  The ranks take the costs' place, the chunk counts in work order that of the prefix.
-    {
-        int per = 1;
-        while (per < 32 && 2 * per * B <= PREP_THREADS) per *= 2;
-        int rank[PREP_MAX_B / PREP_THREADS];
+    // position in the work order by counting the larger keys, four at a time
 #pragma unroll
-        for (int q = 0; q < PREP_MAX_B / PREP_THREADS; ++q) {
-            const int i = q * PREP_THREADS + t, b = i / per;
-            int r = 0;
-            if (b < B) {
-                const int c = sh_cost[b];
-                for (int o = i % per; o < B; o += per) {
-                    const int co = sh_cost[o];
-                    r += (co > c) || (co == c && o < b);
-                }
+    for (int q = 0; q < PASSES; ++q) {
+        const int i = q * PREP_THREADS + t, b = i / per;
+        int r = 0;
+        if (b < B) {
+            const int key = sh_key[b];
+            const int4 *keys = reinterpret_cast<const int4 *>(sh_key);
+            for (int o = i % per; 4 * o < B; o += per) {
+                const int4 k = keys[o];
+                r += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
             }
-            for (int o = 1; o < per; o *= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
-            rank[q] = r;
         }
-        __syncthreads();
+        for (int o = 1; o < per; o *= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
+        rank[q] = r;
+    }
+    __syncthreads();
 #pragma unroll
-        for (int q = 0; q < PREP_MAX_B / PREP_THREADS; ++q) {
-            const int i = q * PREP_THREADS + t, b = i / per;
-            if (b >= B || i % per) continue;
+    for (int q = 0; q < PASSES; ++q) {
+        const int i = q * PREP_THREADS + t, b = i / per;
+        if (b < B && i % per == 0) {
             seq_at_rank[rank[q]] = b;
-            sh_cost[b] = rank[q];
-            sh_tmp[rank[q]] = (int)sh_ns[b];
+            sh_tmp[rank[q]] = ns[q];
         }
     }
     __syncthreads();
     const int total2 = block_exclusive_scan(sh_tmp, B, warp_tot);
     for (int r = t; r < B; r += PREP_THREADS) sorted_start[r] = sh_tmp[r];
     if (t == 0) sorted_start[B] = total2;
-    // per-chunk table in work order, so that the scheduler decodes a work unit with one 32-byte load; again several threads a sequence
+    // per-chunk table in work order, so that the scheduler decodes a work unit with one 32-byte load
     if (unit_tab) {
-        __syncthreads();
-        int per = 1;
-        while (per < 32 && 2 * per * B <= PREP_THREADS) per *= 2;
-        for (int i = t; i < B * per; i += PREP_THREADS) {
-            const int b = i / per, ns = (int)sh_ns[b];
-            // contiguous cache: first token and length; paged cache: first slot of the page table and length
-            const int kv0 = kv_len ? page_indptr[b] : kv_indptr[b];
-            const int L = kv_len ? kv_len[b] : kv_indptr[b + 1] - kv0;
-            const int first = item_start[b];  // written by this block; visible after the barriers above
-            int4 *dst = reinterpret_cast<int4 *>(unit_tab) + 2 * (size_t)sh_tmp[sh_cost[b]];
-            for (int s = i % per; s < ns; s += per) {
-                dst[2 * s] = make_int4(b, s, ns, first);
-                dst[2 * s + 1] = make_int4(kv0, L, 0, 0);
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+            const int i = q * PREP_THREADS + t, b = i / per;
+            if (b >= B) continue;
+            int4 *dst = reinterpret_cast<int4 *>(unit_tab) + 2 * (size_t)sh_tmp[rank[q]];
+            for (int s = i % per; s < ns[q]; s += per) {
+                dst[2 * s] = make_int4(b, s, ns[q], first[q]);
+                dst[2 * s + 1] = make_int4(kv0[q], L[q], 0, 0);
             }
         }
     }

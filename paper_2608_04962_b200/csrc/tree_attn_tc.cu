@@ -78,7 +78,7 @@ struct Cfg {
     static constexpr int THREADS = 32 * (DECODE0 + DECODE_TEAMS * DECODE_WARPS);
     // Registers a thread of each role, where there is decoding: 768 threads get 80 each at the launch, and the groups of four warps share
     // the same sum out anew (the softmax threads keep a tile's probabilities in registers).
-    static constexpr int REGS_LOAD = 56, REGS_SOFT = 120, REGS_OUT = 72, REGS_DECODE = 56;
+    static constexpr int REGS_LOAD = 80, REGS_SOFT = 112, REGS_OUT = 80, REGS_DECODE = 48;
     static_assert(!KV4 || REGS_LOAD + REGS_SOFT * (SOFTMAX_THREADS / 128) + REGS_OUT + REGS_DECODE * DECODE_TEAMS == 80 * (THREADS / 128),
                   "no more registers than the launch gave");
     static constexpr int FULL_ARRIVALS = KV4 ? DECODE_WARPS : 1;  // of a ring stage: the decoding warps, or the loading thread
@@ -94,6 +94,7 @@ struct Cfg {
     // exchange area: the rows' reference maxima as one softmax team leaves them for the other ([2][128] fp32), or
     // the partial row maxima of the pairs (per lane group [2 slots][2 halves][32 lanes] bf16)
     static constexpr int XCH_BYTES = 1024;
+    static constexpr int JOBS = 16 + XCH_BYTES + 2 * 64;  // (in the area behind the barriers)
     static constexpr int EXTRA = BAR_BYTES + 16 + XCH_BYTES + 2 * 64 + 16 * SS;  // barriers, slot/abort/ticket, exchange, ring, slots' jobs
     // hand-over from the softmax warps to the output warps (per row: each team's share of the sum and the
     // reference maximum it is relative to): in global memory, one area per CTA, because shared memory is full
@@ -154,7 +155,7 @@ __device__ __forceinline__ float bf16_bits_to_float(unsigned short b) { return _
 // stages are filled by the decoding teams alone.  A wait on a barrier's parity is right while the waiter is at most one phase behind or
 // ahead: a stage's job waits for the stage's use before to be consumed, so that use's own job must not be still waiting for the
 // one before it.  With SS = 3 slots only two neighbouring jobs of the queue can be in the teams' hands at a time (the one after them needs a slot that
-// the first still holds), and neighbours never have positions four apart but at the very start (K1 V1), where there is no use before.
+// the first still holds), and neighbours' positions are one or three apart, never the RS = 4 of two uses of one stage.
 template <int D, bool TEAMS, bool ONE, bool KV4>
 __global__ void __launch_bounds__(attc::Cfg<D, TEAMS, KV4>::THREADS, 1)
 tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -180,9 +181,9 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     volatile int *tickets = reinterpret_cast<volatile int *>(extra + 8);
     unsigned char *xch_base = extra + 16;
     volatile UnitDesc *ring = reinterpret_cast<volatile UnitDesc *>(extra + 16 + C::XCH_BYTES);  // 2 slots of 64 bytes
-    // 4-bit cache: per staging slot, the ring position it goes to (-1: no more), what it is, and of a tree's tile its KV head and first row
+    // 4-bit cache: per staging slot its job: the ring position it goes to (-1: no more), what it is, and of a tree's tile its KV head and
+    // first row.  (The loading thread calls a page's K and V TREE_K + 2 and TREE_V + 2.)
     enum Job { NO_PAGE, CODES, TREE_K, TREE_V };
-    volatile int *const slot_job = reinterpret_cast<volatile int *>(extra + 16 + C::XCH_BYTES + 2 * 64);
     constexpr bool one_wave = ONE;
     // [l of team 0 | l of team 1 | m of team 0 | m of team 1][128 rows]
     float *hand = a.hand + (size_t)blockIdx.x * C::HAND_FLOATS;
@@ -321,7 +322,121 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             a.lse[((size_t)b * N + n) * a.Hq + hkv * G + g] = (Mx + log2f(lsum)) * 0.6931471805599453f;
     };
 
-    if (warp == 0) {
+    if (KV4 && warp == 0) {
+        // ------------------------------------------------------------------ scheduler + jobs of the decoding teams (4-bit cache)
+        // K0 K1 K2 V0 K3 V1 ..., across units too, as jobs in staging slots: the slot's codes are fetched from here, the tree's tiles by the team
+        // that has the job.  Everything a job needs is kept in registers and counted on.
+        if constexpr (KV4) if (lane == 0) {
+            bool ok = true;
+            uint32_t slot_i = 0, told_i = 0, free_par = 1;  // next slot and its barrier, parity of the wait for it
+            auto post = [&](int kind, int hkv, int at, uint32_t pos) {  // at: the page, or the tree's first row; kind < 0: the end
+                ok = ok && twait(0, bar(C::B_SFREE) + 8u * slot_i, free_par);
+                if (!ok) return;
+                const uint32_t told = bar(C::B_SFILLED) + 8u * told_i;
+                const bool page = kind == TREE_K + 2 || kind == TREE_V + 2, codes = page && at >= 0 && at < a.n_pages;
+                reinterpret_cast<int4 *>(extra + C::JOBS)[slot_i] = make_int4((int)pos, page ? (codes ? CODES : NO_PAGE) : kind, hkv, at);
+                if (codes) {
+                    mbar_arrive_expect_tx(told, C::SLOT_BYTES);
+                    bulk_load(g_s + slot_i * C::SLOT_BYTES, a.pool + (((size_t)at * a.Hkv + hkv) * 2 + (kind == TREE_V + 2)) * C::SLOT_BYTES,
+                              C::SLOT_BYTES, told);
+                } else {
+                    mbar_arrive(told);
+                }
+                if (++slot_i == C::SS) {
+                    slot_i = 0;
+                    free_par ^= 1u;
+                }
+                if (++told_i == C::SF) told_i = 0;
+            };
+            // V trails K by two tiles: the last two K's (kind, KV head, place), and the positions to come
+            int n_pend = 0, kind0 = 0, kind1 = 0, h0 = 0, h1 = 0, at0 = 0, at1 = 0;
+            uint32_t kp = 0, vp = 3;
+            auto next_v = [&]() {
+                post(kind0, h0, at0, vp);
+                vp += 2;
+                kind0 = kind1;
+                h0 = h1;
+                at0 = at1;
+                --n_pend;
+            };
+            auto next_k = [&](bool tree, int hkv, int at) {
+                post(tree ? TREE_K : TREE_K + 2, hkv, at, kp);
+                kp += kp < 2u ? 1u : 2u;
+                if (n_pend == 2) next_v();
+                const int kind = tree ? TREE_V : TREE_V + 2;
+                if (n_pend == 0) kind0 = kind, h0 = hkv, at0 = at;
+                else kind1 = kind, h1 = hkv, at1 = at;
+                ++n_pend;
+            };
+            for (uint32_t u = 0; ok; ++u) {
+                const int slot = (int)(u & 1u);
+                if (!(ok = twait(1, bar(C::B_UEMPTY + slot), ((u >> 1) & 1u) ^ 1u))) break;
+                const int w = u == 0 ? (int)blockIdx.x : (one_wave ? a.total_work : (int)gridDim.x + atomicAdd(a.work_counter, 1));
+                volatile UnitDesc *d = ring + slot;
+                if (w >= a.total_work) {
+                    d->valid = 0;
+                    mbar_arrive(bar(C::B_UFULL + slot));
+                    break;
+                }
+                const int rb = w % a.n_rb, hkv = w / a.n_rb % a.Hkv;
+                const int4 *const row = reinterpret_cast<const int4 *>(a.unit_tab) + 2 * (size_t)(w / a.n_rb / a.Hkv);
+                const int4 e0 = __ldg(row), e1 = __ldg(row + 1);
+                const int b = e0.x, split = e0.y, n_splits = e0.z, slot0 = e1.x, L = e1.y;
+                const int tiles_b = (L + BN - 1) / BN, tps = (tiles_b + n_splits - 1) / n_splits;
+                const int t_lo = min(tiles_b, split * tps), n_kv = min(tiles_b, t_lo + tps) - t_lo;
+                const int has_tree = split == n_splits - 1 ? 1 : 0;
+                const int32_t *const pt = a.page_table + slot0 + t_lo;
+                int pg = n_kv > 0 ? __ldg(pt) : 0;
+                d->valid = 1;
+                d->b = b;
+                d->hkv = hkv;
+                d->rb = rb;
+                d->n_splits = n_splits;
+                d->kv0 = slot0;
+                d->L = L;
+                d->t_lo = t_lo;
+                d->n_it = n_kv + has_tree;
+                d->has_tree = has_tree;
+                d->item = e0.w + split;
+                d->item0 = e0.w;
+                mbar_arrive(bar(C::B_UFULL + slot));  // release: the descriptor is visible to whoever acquires
+                const int qb = (int)(u % QS);
+                if (u >= (uint32_t)QS && !(ok = twait(2, bar(C::B_QFREE + qb), (u / QS - 1u) & 1u))) break;
+                auto load_q = [&]() {
+                    mbar_arrive_expect_tx(bar(C::B_QFULL + qb), (uint32_t)(C::NBOX * 128 * a.rows_per_block));
+#pragma unroll
+                    for (int bx = 0; bx < C::NBOX; ++bx)
+                        tma_load_3d(q_s + qb * C::Q_BYTES + bx * BOX_BYTES, &tmQ, bx * 64, hkv * G,
+                                    b * N + rb * a.nodes_per_block, bar(C::B_QFULL + qb));
+                };
+                // early cache loads, as below: the first unit's first pages go out before the kernel in front of this one has finished
+                bool q_pending = early && u == 0;
+                auto settle = [&]() {
+                    asm volatile("griddepcontrol.wait;" ::: "memory");
+                    load_q();
+                    q_pending = false;
+                };
+                if (!q_pending) load_q();
+                int pg1 = n_kv > 1 ? __ldg(pt + 1) : 0;
+                for (int it = 0; it < n_kv && ok; ++it) {
+                    const int pg2 = it + 2 < n_kv ? __ldg(pt + it + 2) : 0;
+                    if (q_pending && it >= 3) settle();
+                    next_k(false, hkv, pg);
+                    pg = pg1;
+                    pg1 = pg2;
+                }
+                if (q_pending) settle();
+                if (has_tree && ok) next_k(true, hkv, b * N);
+                // (the unit's last V's follow the next unit's first K's.  Ahead of those, or with the next unit asked for before this one's last
+                // tile, they kept the teams from the tiles that were needed next: 204 us became 206 to 215 on 256 sequences, 56 rows.)
+            }
+            // (a thread that left the loop early has not waited yet; the counters touched at the end of the kernel are cleared by the
+            // launch before this one)
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            while (ok && n_pend > 0) next_v();
+            for (int i = 0; i < C::DECODE_TEAMS && ok; ++i) post(NO_PAGE, 0, 0, 0xffffffffu);  // the end, once for each team
+        }
+    } else if (warp == 0) {
         // ------------------------------------------------------------------ scheduler + TMA producer
         if (lane == 0) {
             bool ok = true;
@@ -330,34 +445,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const CUtensorMap *pv_map[2];
             int pv_h[2], pv_tok[2];
             int n_pend = 0;
-            // 4-bit cache: the job for ring position pos (codes of a page: K where kind is TREE_K, else V; or the tree's tile) into the next slot
-            uint32_t staged = 0;
-            auto filled = [&]() { return bar(C::B_SFILLED + (int)(staged % (C::SF ? C::SF : 1))); };
-            auto slot_free = [&]() { return bar(C::B_SFREE + (int)(staged % (C::SS ? C::SS : 1))); };
-            auto slot_parity = [&]() { return ((staged / (C::SS ? C::SS : 1)) & 1u) ^ 1u; };
-            auto post = [&](bool tree, int kind, int hkv, int at, uint32_t pos) -> bool {
-                if constexpr (KV4) {
-                    const int s = (int)(staged % C::SS);
-                    if (!twait(5, slot_free(), slot_parity())) return false;
-                    const uint32_t told = filled();
-                    ++staged;
-                    const bool codes = !tree && at >= 0 && at < a.n_pages;
-                    slot_job[4 * s] = (int)pos;
-                    slot_job[4 * s + 1] = tree ? kind : codes ? CODES : NO_PAGE;
-                    slot_job[4 * s + 2] = hkv;
-                    slot_job[4 * s + 3] = at;
-                    if (codes) {
-                        mbar_arrive_expect_tx(told, C::SLOT_BYTES);
-                        bulk_load(g_s + s * C::SLOT_BYTES, a.pool + (((size_t)at * a.Hkv + hkv) * 2 + (kind == TREE_V)) * C::SLOT_BYTES,
-                                  C::SLOT_BYTES, told);
-                    } else {
-                        mbar_arrive(told);
-                    }
-                }
-                return true;
-            };
             auto load_v = [&](const CUtensorMap *mv, int hkv, int tok) -> bool {
-                if (KV4) return post(mv == &tmVt, TREE_V, hkv, tok, v_pos(vt++));  // (tok: the page, or the tree's first row)
                 int s;
                 uint32_t ph;
                 v_slot(vt, s, ph);
@@ -443,32 +531,24 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 int pg0 = (pt && n_kv > 0) ? __ldg(pt) : 0, pg1 = (pt && n_kv > 1) ? __ldg(pt + 1) : 0;
                 for (int it = 0; it < n_it && ok; ++it) {
                     const int pg2 = (pt && it + 2 < n_kv) ? __ldg(pt + it + 2) : 0;
+                    int s;
+                    uint32_t kph;
+                    k_slot(kt, s, kph);
+                    if (!twait(3, bar(C::B_EMPTY + s), kph ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
                     const bool tree = has_tree && (it == n_it - 1);
-                    const int tok = tree ? b * N : (KV4 ? pg0 : pt ? pg0 * BN : kv0 + (t_lo + it) * BN);
+                    if (q_pending && (tree || it >= 3)) settle();
+                    const int tok = tree ? b * N : (pt ? pg0 * BN : kv0 + (t_lo + it) * BN);
                     pg0 = pg1;
                     pg1 = pg2;
-                    if constexpr (KV4) {
-                        if (q_pending && (tree || it >= 3)) settle();
-                        if (!post(tree, TREE_K, hkv, tok, k_pos(kt))) {
-                            ok = false;
-                            break;
-                        }
-                    } else {
-                        int s;
-                        uint32_t kph;
-                        k_slot(kt, s, kph);
-                        if (!twait(3, bar(C::B_EMPTY + s), kph ^ 1u)) {
-                            ok = false;
-                            break;
-                        }
-                        if (q_pending && (tree || it >= 3)) settle();
-                        const CUtensorMap *mk = tree ? &tmKt : &tmK;
-                        const uint32_t dst = stage_addr(s);
-                        mbar_arrive_expect_tx(bar(C::B_FULL + s), C::KV_BYTES);
+                    const CUtensorMap *mk = tree ? &tmKt : &tmK;
+                    const uint32_t dst = stage_addr(s);
+                    mbar_arrive_expect_tx(bar(C::B_FULL + s), C::KV_BYTES);
 #pragma unroll
-                        for (int bx = 0; bx < C::NBOX; ++bx)
-                            tma_load_3d(dst + bx * BOX_BYTES, mk, bx * 64, hkv, tok, bar(C::B_FULL + s));
-                    }
+                    for (int bx = 0; bx < C::NBOX; ++bx)
+                        tma_load_3d(dst + bx * BOX_BYTES, mk, bx * 64, hkv, tok, bar(C::B_FULL + s));
                     ++kt;
                     if (n_pend == 2) {
                         ok = load_v(pv_map[0], pv_h[0], pv_tok[0]);
@@ -489,7 +569,6 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     int s;
                     uint32_t ph;
                     v_slot(vt, s, ph);
-                    if (KV4) return mbar_test_wait(slot_free(), slot_parity());
                     return mbar_test_wait(bar(C::B_EMPTY + s), ph ^ 1u);
                 };
                 while (ok && n_pend > 0 && v_stage_free()) {
@@ -505,16 +584,6 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             asm volatile("griddepcontrol.wait;" ::: "memory");
             // flush the V tiles still pending (the last two tiles of the last unit)
             for (int i = 0; i < n_pend && ok; ++i) ok = load_v(pv_map[i], pv_h[i], pv_tok[i]);
-            if constexpr (KV4) {
-                for (int i = 0; i < C::DECODE_TEAMS && ok; ++i) {  // the end, once for each team
-                    const int s = (int)(staged % C::SS);
-                    ok = twait(6, slot_free(), slot_parity());
-                    if (!ok) break;
-                    slot_job[4 * s] = -1;
-                    mbar_arrive(filled());
-                    ++staged;
-                }
-            }
             if (!ok) {
                 // aborting: give copies in flight time to land before the CTA goes away
                 const unsigned long long t0 = globaltimer_ns();
@@ -638,7 +707,8 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 ok = twait(0, bar(C::B_SFILLED + (int)(n % C::SF)), (n / C::SF) & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const int pos = slot_job[4 * s], kind = slot_job[4 * s + 1];
+                const int4 job = *reinterpret_cast<const int4 *>(extra + C::JOBS + 16 * s);
+                const int pos = job.x, kind = job.y;
                 if (pos < 0) break;
                 const int st = pos % RS;
                 ok = twait(1, bar(C::B_EMPTY + st), (((uint32_t)pos / RS) & 1u) ^ 1u);
@@ -651,7 +721,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                             mbar_arrive_expect_tx(bar(C::B_FULL + st), C::KV_BYTES);
 #pragma unroll
                             for (int bx = 0; bx < C::NBOX; ++bx)
-                                tma_load_3d(stage_addr(st) + bx * BOX_BYTES, map, bx * 64, slot_job[4 * s + 2], slot_job[4 * s + 3],
+                                tma_load_3d(stage_addr(st) + bx * BOX_BYTES, map, bx * 64, job.z, job.w,
                                             bar(C::B_FULL + st));
                         } else {
                             mbar_arrive(bar(C::B_FULL + st));
