@@ -11,16 +11,22 @@
 
 namespace specroll {
 
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
 // Codes of eight elements, and the block's scale byte, from the four threads that share the block.
 __device__ __forceinline__ uint32_t kv4_encode(const uint4 &x, uint32_t &scale) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     // magnitudes as integers: 0x7f80 is infinity, above it NaN
-    uint32_t m2 = 0u;
+    uint32_t m2 = w[0] & 0x7fff7fffu;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m2 = __vmaxu2(m2, w[i] & 0x7fff7fffu);
+    for (int i = 1; i < 4; ++i) m2 = max_u16x2(m2, w[i] & 0x7fff7fffu);
+    m2 = max_u16x2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
+    m2 = max_u16x2(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
     uint32_t top = max(m2 & 0xffffu, m2 >> 16);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     float v[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -41,8 +47,9 @@ __device__ __forceinline__ uint32_t kv4_encode(const uint4 &x, uint32_t &scale) 
         mx = fmaxf(mx, __shfl_xor_sync(four, mx, 2));
         top = __float_as_uint(mx) >> 16;
     }
-    const float t = __fdiv_rn(__uint_as_float(top << 16), 7.0f);
-    int c = (int)((__float_as_uint(t) + (1u << 19)) >> 20) - (int)(KV4_EXP0 >> 4);
+    // (128 + M) 2^(E - 134) over 7 to four significant bits, halves up: (128 + M) / 14 or, from 224 on, / 28, rounded
+    const int M = (int)(top & 127u), r = M < 96 ? ((135 + M) * 4682 >> 16) - 8 : (142 + M) * 2341 >> 16;
+    int c = 8 * ((int)(top >> 7) - 110) + r;
     if (c > 255) {
         c = 255;
         clip = true;
@@ -53,9 +60,11 @@ __device__ __forceinline__ uint32_t kv4_encode(const uint4 &x, uint32_t &scale) 
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fminf(fmaxf(v[i], -8.0f * s), 7.0f * s);
     }
-    // The reciprocal is taken a little too large, so that halves, which are exact quotients, go away from zero; every other
-    // quotient of an 8-bit and a 4-bit significand is further than 2^-12 from a half.  1.5 2^23 + 8 leaves code = q + 8.
-    const float inv = __fdiv_rn(1.0f + 0x1p-21f, s);
+    // The reciprocal (good to 2^-23) is taken a little too large, so that halves, which are exact quotients, go away from zero; every
+    // other quotient of an 8-bit and a 4-bit significand is further than 2^-12 from a half.  1.5 2^23 + 8 leaves code = q + 8.
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    inv *= 1.0f + 0x1p-21f;
     uint32_t y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = __float_as_uint(fmaf(v[i], inv, 12582920.0f));
@@ -73,96 +82,99 @@ __device__ __forceinline__ void kv4_put(uint8_t *tile, int row, int at, uint32_t
 
 constexpr int KV4_THREADS = 256, KV4_EACH = 4;  // words of 16 bytes of bf16 that a thread takes side by side
 
-// What the two kernels by slot share out: lines (a token's K or V of all heads: Hkv D / 8 words), `lines` to a block, so that a block has
-// about KV4_THREADS x KV4_EACH words; a warp reads and writes contiguous memory on the bf16 side.
-struct Kv4Lines {
+// What the two kernels by slot share out.  A thread has one word of K or of V of its tokens for good (a token has `columns` = 2 Hkv D / 8
+// words; 256 threads are 256 / columns tokens side by side, or a part of one, by blockIdx.y) and goes through tokens, so that everything
+// but the slot is found once, in 32 bits (with places in 64 bits found for every word the kernels took 160 instructions a word and were
+// bound by them).  A warp reads and writes contiguous memory on the bf16 side.
+struct Kv4Tokens {
     const long long *slots;
-    long long n_lines, n_slots;  // 2 T; slots of the pool
-    int32_t lines, words, Hkv;   // lines of a block, words of a line
-    uint32_t by_words;           // floor(2^32 / words) + 1: a block's word number over `words` by multiplication
+    unsigned long long n_slots;  // slots of the pool
+    uint32_t T, columns, side, each, page_bytes;  // tokens; words of a token; tokens side by side; tokens of a thread; bytes of a page
 };
 
-struct Kv4Word {
-    long long tok, slot;
-    int v, word;  // K or V; word of the line
-    bool in;
-};
-__device__ __forceinline__ Kv4Word kv4_word_of(const Kv4Lines &a, uint32_t i) {
-    const uint32_t l = __umulhi(i, a.by_words);
-    const long long line = (long long)blockIdx.x * a.lines + l;
-    Kv4Word w;
-    w.in = l < (uint32_t)a.lines && line < a.n_lines;
-    w.tok = line >> 1;
-    w.v = (int)(line & 1);
-    w.word = (int)(i - l * a.words);
-    w.slot = w.in ? __ldg(a.slots + w.tok) : -1;
-    return w;
-}
-// Tile of a word, and its token's row there.
 template <int D>
-__device__ __forceinline__ long long kv4_tile_of(const Kv4Lines &a, const Kv4Word &w) {
-    return (((w.slot >> 7) * a.Hkv + w.word / (D / 8)) * 2 + w.v) * (long long)Kv4<D>::TILE;
-}
+struct Kv4Column {
+    uint32_t tok, word, v;  // first token, word of K or V
+    uint32_t at, sat;       // places of the word's codes and scale in row 0 of the head's tile, from the page's first byte
+    bool on;
+    __device__ __forceinline__ explicit Kv4Column(const Kv4Tokens &a) {
+        const uint32_t l = a.columns < KV4_THREADS ? threadIdx.x / a.columns : 0u;
+        const uint32_t col = threadIdx.x - l * a.columns + blockIdx.y * KV4_THREADS, words = a.columns / 2;
+        on = l < a.side && col < a.columns;
+        v = col >= words;
+        word = v ? col - words : col;
+        tok = blockIdx.x * a.side * a.each + l;
+        const uint32_t tile = (word / (D / 8) * 2 + v) * Kv4<D>::TILE, of_head = word % (D / 8);
+        at = tile + of_head * 4;
+        sat = tile + Kv4<D>::CODES + of_head / 4;
+    }
+    __device__ __forceinline__ bool has(const Kv4Tokens &a, uint32_t q) const { return on && q < a.each && tok + q * a.side < a.T; }
+    __device__ __forceinline__ unsigned long long slot(const Kv4Tokens &a, uint32_t q) const {
+        return has(a, q) ? (unsigned long long)__ldg(a.slots + tok + q * a.side) : ~0ull;
+    }
+};
 static_assert(SPECROLL_PAGE_TOKENS == 128, "slot >> 7");
 
 template <int D>
 __global__ void __launch_bounds__(KV4_THREADS)
-kv4_store_kernel(const uint4 *__restrict__ K, const uint4 *__restrict__ V, const Kv4Lines a, uint8_t *__restrict__ pool,
+kv4_store_kernel(const uint4 *__restrict__ K, const uint4 *__restrict__ V, const Kv4Tokens a, uint8_t *__restrict__ pool,
                  int32_t *__restrict__ status) {
     pdl_wait();
     pdl_launch_dependents();
-    for (uint32_t i0 = threadIdx.x; i0 - threadIdx.x < (uint32_t)(a.lines * a.words); i0 += KV4_THREADS * KV4_EACH) {
-        Kv4Word w[KV4_EACH];
-        uint4 x[KV4_EACH];
+    const Kv4Column<D> c(a);
+    const uint4 *const src = (c.v ? V : K) + c.word;
+    unsigned long long slot[KV4_EACH];
+    uint4 x[KV4_EACH];
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) w[q] = kv4_word_of(a, i0 + q * KV4_THREADS);
+    for (uint32_t q = 0; q < KV4_EACH; ++q) slot[q] = c.slot(a, q);
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) {
-            const bool ok = w[q].slot >= 0 && w[q].slot < a.n_slots;
-            x[q] = ok ? ld_nc_v4((w[q].v ? V : K) + w[q].tok * a.words + w[q].word) : make_uint4(0u, 0u, 0u, 0u);
-        }
+    for (uint32_t q = 0; q < KV4_EACH; ++q)
+        x[q] = slot[q] < a.n_slots ? ld_nc_v4(src + (unsigned long long)(c.tok + q * a.side) * (a.columns / 2)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) {
-            uint32_t scale;
-            const uint32_t codes = kv4_encode(x[q], scale);  // (four threads a block of 32, all in it together)
-            if (w[q].slot >= 0 && w[q].slot < a.n_slots)
-                kv4_put<D>(pool + kv4_tile_of<D>(a, w[q]), (int)(w[q].slot & 127), w[q].word % (D / 8), codes, scale);
-            else if (w[q].in && w[q].slot >= 0 && status && w[q].word == 0)
-                atomicExch(status, SPECROLL_ELIMIT);
+    for (uint32_t q = 0; q < KV4_EACH; ++q) {
+        uint32_t scale;
+        const uint32_t codes = kv4_encode(x[q], scale);  // (four threads a block of 32, all in it together)
+        if (slot[q] < a.n_slots) {
+            uint8_t *const page = pool + (unsigned long long)(uint32_t)(slot[q] >> 7) * a.page_bytes;
+            const uint32_t row = (uint32_t)slot[q] & 127u;
+            *reinterpret_cast<uint32_t *>(page + (c.at + row * Kv4<D>::ROW)) = codes;
+            if ((c.word & 3) == 0) page[c.sat + row * Kv4<D>::SROW] = (uint8_t)scale;
+        } else if ((long long)slot[q] >= 0 && status && c.word == 0) {
+            atomicExch(status, SPECROLL_ELIMIT);
         }
     }
 }
 
 template <int D>
 __global__ void __launch_bounds__(KV4_THREADS)
-kv4_load_kernel(const uint8_t *__restrict__ pool, const Kv4Lines a, uint4 *__restrict__ K, uint4 *__restrict__ V, int32_t *__restrict__ status) {
+kv4_load_kernel(const uint8_t *__restrict__ pool, const Kv4Tokens a, uint4 *__restrict__ K, uint4 *__restrict__ V, int32_t *__restrict__ status) {
     pdl_wait();
     pdl_launch_dependents();
-    for (uint32_t i0 = threadIdx.x; i0 - threadIdx.x < (uint32_t)(a.lines * a.words); i0 += KV4_THREADS * KV4_EACH) {
-        Kv4Word w[KV4_EACH];
-        uint32_t codes[KV4_EACH], scale[KV4_EACH];
+    const Kv4Column<D> c(a);
+    uint4 *const dst = (c.v ? V : K) + c.word;
+    unsigned long long slot[KV4_EACH];
+    uint32_t codes[KV4_EACH], scale[KV4_EACH];
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) w[q] = kv4_word_of(a, i0 + q * KV4_THREADS);
+    for (uint32_t q = 0; q < KV4_EACH; ++q) slot[q] = c.slot(a, q);
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) {
-            codes[q] = 0x88888888u;  // (zeros)
-            scale[q] = 0u;
-            if (w[q].slot >= 0 && w[q].slot < a.n_slots) {
-                const uint8_t *tile = pool + kv4_tile_of<D>(a, w[q]);
-                const int row = (int)(w[q].slot & 127), at = w[q].word % (D / 8);
-                codes[q] = __ldg(reinterpret_cast<const uint32_t *>(tile + row * Kv4<D>::ROW) + at);
-                scale[q] = __ldg(tile + Kv4<D>::CODES + row * Kv4<D>::SROW + (at >> 2));
-            } else if (w[q].in && w[q].slot >= 0 && status && w[q].word == 0) {
-                atomicExch(status, SPECROLL_ELIMIT);
-            }
+    for (uint32_t q = 0; q < KV4_EACH; ++q) {
+        codes[q] = 0x88888888u;  // (zeros)
+        scale[q] = 0u;
+        if (slot[q] < a.n_slots) {
+            const uint8_t *const page = pool + (unsigned long long)(uint32_t)(slot[q] >> 7) * a.page_bytes;
+            const uint32_t row = (uint32_t)slot[q] & 127u;
+            codes[q] = __ldg(reinterpret_cast<const uint32_t *>(page + (c.at + row * Kv4<D>::ROW)));
+            scale[q] = __ldg(page + (c.sat + row * Kv4<D>::SROW));
+        } else if ((long long)slot[q] >= 0 && status && c.word == 0) {
+            atomicExch(status, SPECROLL_ELIMIT);
         }
+    }
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) {
-            uint32_t r[4];
-            const uint32_t s = kv4_scale_twice(scale[q]);
-            kv4_word(codes[q], s, kv4_offset(s), r);
-            if (w[q].in) __stcs((w[q].v ? V : K) + w[q].tok * a.words + w[q].word, make_uint4(r[0], r[1], r[2], r[3]));
-        }
+    for (uint32_t q = 0; q < KV4_EACH; ++q) {
+        uint32_t r[4];
+        const uint32_t s = kv4_scale_twice(scale[q]);
+        kv4_word(codes[q], s, kv4_offset(s), r);
+        if (c.has(a, q)) __stcs(dst + (unsigned long long)(c.tok + q * a.side) * (a.columns / 2), make_uint4(r[0], r[1], r[2], r[3]));
     }
 }
 
@@ -257,33 +269,34 @@ extern "C" size_t specroll_kv4_tile_bytes(int32_t D) {
     return D == 64 ? Kv4<64>::TILE : D == 128 ? Kv4<128>::TILE : 0;
 }
 
-// What the two calls by slot share: the checks, and how the lines are shared out (*blocks = 0: nothing to do).
+// What the two calls by slot share: the checks, and how the tokens are shared out (grid.x = 0: nothing to do).
 static int by_slot(int64_t T, int32_t Hkv, int32_t D, const void *K, const void *V, const int64_t *slots, const void *pool, int64_t n_pages,
-                   Kv4Lines *a, unsigned *blocks) {
-    *blocks = 0;
+                   Kv4Tokens *a, dim3 *grid) {
+    grid->x = 0;
     if (T < 0 || T > (1LL << 30) || Hkv < 1 || Hkv > 4096 || (D != 64 && D != 128) || n_pages < 0 || n_pages > (1LL << 24)) return SPECROLL_EINVAL;
     if (T == 0) return SPECROLL_OK;  // (no tokens have empty arrays: their pointers may be NULL)
     if (!K || !V || !slots || (n_pages > 0 && !pool)) return SPECROLL_EINVAL;
     if (!aligned16(K) || !aligned16(V) || !aligned16(pool)) return SPECROLL_EALIGN;
-    const int words = Hkv * (D / 8), most = KV4_THREADS * KV4_EACH;
     a->slots = reinterpret_cast<const long long *>(slots);
-    a->n_lines = 2 * T;
-    a->n_slots = (long long)n_pages * SPECROLL_PAGE_TOKENS;
-    a->words = words;
-    a->lines = words < most ? most / words : 1;
-    a->Hkv = Hkv;
-    a->by_words = (uint32_t)((1ULL << 32) / (unsigned)words + 1);
-    *blocks = (unsigned)((a->n_lines + a->lines - 1) / a->lines);
+    a->n_slots = (unsigned long long)n_pages * SPECROLL_PAGE_TOKENS;
+    a->T = (uint32_t)T;
+    a->columns = (uint32_t)(2 * Hkv * (D / 8));
+    a->page_bytes = (uint32_t)(Hkv * 2 * specroll_kv4_tile_bytes(D));
+    a->side = std::max(1u, KV4_THREADS / a->columns);
+    // one word a thread while that is less than a wave of blocks: few tokens are a chain of latencies
+    a->each = T * a->columns > 148LL * 8 * KV4_THREADS ? KV4_EACH : 1;
+    grid->x = (unsigned)((T + a->side * a->each - 1) / (a->side * a->each));
+    grid->y = (a->columns + KV4_THREADS - 1) / KV4_THREADS;
     return SPECROLL_OK;
 }
 
 extern "C" int specroll_kv4_store(int64_t T, int32_t Hkv, int32_t D, const void *K, const void *V, const int64_t *slot_map, void *pool,
                                   int64_t n_pages, int32_t *status, void *cuda_stream) {
-    Kv4Lines a;
-    unsigned blocks = 0;
-    const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &blocks);
-    if (rc != SPECROLL_OK || !blocks) return rc;
-    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_store_kernel<128> : kv4_store_kernel<64>, dim3(blocks), dim3(KV4_THREADS), 0,
+    Kv4Tokens a;
+    dim3 grid;
+    const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &grid);
+    if (rc != SPECROLL_OK || grid.x == 0) return rc;
+    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_store_kernel<128> : kv4_store_kernel<64>, grid, dim3(KV4_THREADS), 0,
                                  static_cast<cudaStream_t>(cuda_stream), static_cast<const uint4 *>(K), static_cast<const uint4 *>(V), a,
                                  static_cast<uint8_t *>(pool), status));
     return SPECROLL_OK;
@@ -291,11 +304,11 @@ extern "C" int specroll_kv4_store(int64_t T, int32_t Hkv, int32_t D, const void 
 
 extern "C" int specroll_kv4_load(int64_t T, int32_t Hkv, int32_t D, const void *pool, int64_t n_pages, const int64_t *slot_map, void *K,
                                  void *V, int32_t *status, void *cuda_stream) {
-    Kv4Lines a;
-    unsigned blocks = 0;
-    const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &blocks);
-    if (rc != SPECROLL_OK || !blocks) return rc;
-    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_load_kernel<128> : kv4_load_kernel<64>, dim3(blocks), dim3(KV4_THREADS), 0,
+    Kv4Tokens a;
+    dim3 grid;
+    const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &grid);
+    if (rc != SPECROLL_OK || grid.x == 0) return rc;
+    SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_load_kernel<128> : kv4_load_kernel<64>, grid, dim3(KV4_THREADS), 0,
                                  static_cast<cudaStream_t>(cuda_stream), static_cast<const uint8_t *>(pool), a, static_cast<uint4 *>(K),
                                  static_cast<uint4 *>(V), status));
     return SPECROLL_OK;
