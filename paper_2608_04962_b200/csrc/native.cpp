@@ -157,8 +157,8 @@ struct Ref {
 };
 
 // ---- results
-at::Tensor alloc(std::initializer_list<int64_t> size, at::ScalarType dtype, const at::Tensor &like) {
-    if (!g_alloc) return at::empty(at::IntArrayRef(size), at::TensorOptions().dtype(dtype).device(like.device()));
+at::Tensor alloc(at::IntArrayRef size, at::ScalarType dtype, const at::Tensor &like) {
+    if (!g_alloc) return at::empty(size, at::TensorOptions().dtype(dtype).device(like.device()));
     PyObject *shp = PyTuple_New((Py_ssize_t)size.size());
     Py_ssize_t i = 0;
     for (int64_t s : size) PyTuple_SET_ITEM(shp, i++, PyLong_FromLongLong(s));
@@ -174,6 +174,33 @@ at::Tensor alloc(std::initializer_list<int64_t> size, at::ScalarType dtype, cons
 }
 at::Tensor alloc_bytes(size_t n, const at::Tensor &like) {
     return alloc({(int64_t)(n < 256 ? 256 : n)}, U8, like);
+}
+// Several outputs that belong together (a page plan's arrays, K and V) from one allocation, each on a 256-byte boundary of it: an
+// allocation takes a microsecond or more of the host, a tensor over a part of one a tenth.  With a replaced allocator, one by one.
+struct Part {
+    at::IntArrayRef size;
+    at::ScalarType dtype;
+};
+template <size_t N>
+void alloc_parts(const Part (&parts)[N], const at::Tensor &like, at::Tensor (&out)[N]) {
+    size_t bytes[N], total = 0;
+    for (size_t i = 0; i < N; ++i) {
+        bytes[i] = (size_t)c10::multiply_integers(parts[i].size) * c10::elementSize(parts[i].dtype);
+        total += (bytes[i] + 255) / 256 * 256;
+    }
+    if (g_alloc || total == 0) {
+        for (size_t i = 0; i < N; ++i) out[i] = alloc(parts[i].size, parts[i].dtype, like);
+        return;
+    }
+    const at::Tensor base = at::empty({(int64_t)total}, at::TensorOptions().dtype(U8).device(like.device()));
+    size_t at = 0;
+    for (size_t i = 0; i < N; ++i) {
+        auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(parts[i].dtype));
+        impl->set_storage_offset((int64_t)(at / c10::elementSize(parts[i].dtype)));
+        impl->set_sizes_contiguous(parts[i].size);
+        out[i] = at::Tensor(std::move(impl));
+        at += (bytes[i] + 255) / 256 * 256;
+    }
 }
 // The workspace of a call: the caller's, or a new one of `n` bytes.
 at::Tensor workspace(PyObject *o, size_t n, const at::Tensor &like) {
@@ -396,12 +423,26 @@ PyObject *page_plan(PyObject *const *a) {
         }
     }
     Out out(a[9]);
-    auto *ot = (int32_t *)out.get("page_table", {table_cap}, I32, kl);
-    auto *oi = (int32_t *)out.get("page_indptr", {B + 1}, I32, kl);
-    auto *ok = (int32_t *)out.get("tok_indptr", {B + 1}, I32, kl);
-    auto *os = (int64_t *)out.get("slot_map", {slot_cap}, I64, kl);
-    auto *of = (int32_t *)out.get("free_list", {fl.numel()}, I32, kl);
-    auto *on = (int32_t *)out.get("n_free", {1}, I32, kl);
+    int32_t *ot, *oi, *ok, *of, *on;
+    int64_t *os;
+    if (a[9] != Py_None) {
+        ot = (int32_t *)out.get("page_table", {table_cap}, I32, kl);
+        oi = (int32_t *)out.get("page_indptr", {B + 1}, I32, kl);
+        ok = (int32_t *)out.get("tok_indptr", {B + 1}, I32, kl);
+        os = (int64_t *)out.get("slot_map", {slot_cap}, I64, kl);
+        of = (int32_t *)out.get("free_list", {fl.numel()}, I32, kl);
+        on = (int32_t *)out.get("n_free", {1}, I32, kl);
+    } else {
+        const int64_t n[6] = {table_cap, B + 1, B + 1, slot_cap, fl.numel(), 1};
+        at::Tensor t[6];
+        alloc_parts<6>({{{n + 0, 1}, I32}, {{n + 1, 1}, I32}, {{n + 2, 1}, I32}, {{n + 3, 1}, I64}, {{n + 4, 1}, I32}, {{n + 5, 1}, I32}}, kl, t);
+        ot = (int32_t *)out.put("page_table", t[0]);
+        oi = (int32_t *)out.put("page_indptr", t[1]);
+        ok = (int32_t *)out.put("tok_indptr", t[2]);
+        os = (int64_t *)out.put("slot_map", t[3]);
+        of = (int32_t *)out.put("free_list", t[4]);
+        on = (int32_t *)out.put("n_free", t[5]);
+    }
     CALL(specroll_page_plan, (int32_t)B, pl, pa, ppt, (int32_t)pt.numel(), ppi, pf, (int32_t)fl.numel(), pn, (int32_t)table_cap, slot_cap, ot, oi, ok, os, of,
          on, ps);
     return out.release();
@@ -436,7 +477,8 @@ PyObject *kv4_load(PyObject *const *a) {
             if (!shape(kv[i], {T, Hkv, D})) fail("kv4_load: out must be [T, Hkv, D]");
         }
     } else {
-        for (auto &t : kv) t = alloc({T, Hkv, D}, BF16, pool);
+        const int64_t size[3] = {T, Hkv, D};
+        alloc_parts<2>({{{size, 3}, BF16}, {{size, 3}, BF16}}, pool, kv);
     }
     const at::Tensor *st = tensor(a[3], "status");
     if (st && st->numel() != 1) fail("kv4_load: status must be one word");

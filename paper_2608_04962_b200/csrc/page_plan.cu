@@ -10,7 +10,7 @@
 
 namespace specroll {
 
-constexpr int PLAN_MAX_B = 4096, PLAN_THREADS = 512;
+constexpr int PLAN_MAX_B = 4096, PLAN_THREADS = 256;
 constexpr int PLAN_PER = 4;  // neighbouring slots a thread writes at a time (two 16-byte stores)
 constexpr uint32_t PLAN_SAT = 0x7fffffffu;
 
@@ -120,30 +120,38 @@ page_plan_kernel(const PagePlanArgs a) {
     auto new_page = [&](long long j) -> int { return j < nf ? __ldg(a.free_list + j) : -1; };
     auto page_of = [&](int b, int i, int had) -> int { return i < had ? old_page(b, i) : new_page((long long)takes[b] + i - had); };
 
-    const long long stride = (long long)gridDim.x * PLAN_THREADS, me = (long long)blockIdx.x * PLAN_THREADS + t;
-    for (long long i = me; i <= B; i += stride) {
-        a.indptr_out[i] = owns[i];
-        a.tok_indptr[i] = toks[i];
-    }
-    for (long long i = me; i < a.table_cap; i += stride) {
-        int page = -1;
-        if (i < tot[0]) {
-            const int b = plan_seq_of(owns, B, (int)i);
-            page = page_of(b, (int)i - owns[b], hads[b]);
+    // one index for all entries (index rows, the table, the free list, groups of slots), so that a thread has one chain of latencies
+    const long long n_slots = min((long long)tot[1], min(a.slot_cap, (long long)PLAN_SAT));
+    const long long to_table = B + 1, to_free = to_table + a.table_cap, to_slots = to_free + a.free_cap;
+    const long long end_of_all = to_slots + (a.slot_cap + PLAN_PER - 1) / PLAN_PER;
+    for (long long e = (long long)blockIdx.x * PLAN_THREADS + t; e < end_of_all; e += (long long)gridDim.x * PLAN_THREADS) {
+        if (e < to_table) {
+            a.indptr_out[e] = owns[e];
+            a.tok_indptr[e] = toks[e];
+            continue;
         }
-        a.table_out[i] = page;
-    }
-    for (long long i = me; i < a.free_cap; i += stride) {
-        int page = -1;
-        if (i < left) page = new_page((long long)tot[2] + i);
-        else if (i < free_after) {
-            const int at = (int)(i - left), b = plan_seq_of(gives, B, at);
-            page = old_page(b, at - gives[b]);
+        if (e < to_free) {
+            const long long i = e - to_table;
+            int page = -1;
+            if (i < tot[0]) {
+                const int b = plan_seq_of(owns, B, (int)i);
+                page = page_of(b, (int)i - owns[b], hads[b]);
+            }
+            a.table_out[i] = page;
+            continue;
         }
-        a.free_out[i] = page;
-    }
-    const long long n_slots = min(a.slot_cap, (long long)PLAN_SAT);
-    for (long long i0 = me * PLAN_PER; i0 < a.slot_cap; i0 += stride * PLAN_PER) {
+        if (e < to_slots) {
+            const long long i = e - to_free;
+            int page = -1;
+            if (i < left) page = new_page((long long)tot[2] + i);
+            else if (i < free_after) {
+                const int at = (int)(i - left), b = plan_seq_of(gives, B, at);
+                page = old_page(b, at - gives[b]);
+            }
+            a.free_out[i] = page;
+            continue;
+        }
+        const long long i0 = (e - to_slots) * PLAN_PER;
         long long out[PLAN_PER];
         int b = -1, had = 0, end = -1, page = -1;
         long long first = 0, in_page = -1;  // the sequence's first new position less its first new token; the page held
@@ -151,7 +159,7 @@ page_plan_kernel(const PagePlanArgs a) {
         for (int q = 0; q < PLAN_PER; ++q) {
             const long long i = i0 + q;
             out[q] = -1;
-            if (i >= min((long long)tot[1], n_slots)) continue;
+            if (i >= n_slots) continue;
             if (i >= end) {
                 b = plan_seq_of(toks, B, (int)i);
                 end = toks[b + 1];
@@ -206,9 +214,10 @@ extern "C" int specroll_page_plan(int32_t B, const int32_t *kv_len, const int32_
     const PagePlanArgs a = {kv_len, add, page_table, page_indptr, free_list, n_free, page_table_out, page_indptr_out, tok_indptr,
                             free_list_out, n_free_out, status, reinterpret_cast<long long *>(slot_map), B, n_table, free_cap, table_cap,
                             slot_cap};
-    // as many blocks as give every thread an entry or four neighbouring slots, up to two a multiprocessor
-    const long long most = std::max<long long>({(long long)B + 1, table_cap, free_cap, (slot_cap + PLAN_PER - 1) / PLAN_PER});
-    const long long want = std::min<long long>((most + PLAN_THREADS - 1) / PLAN_THREADS, 2LL * n_sm);
+    // as many blocks as give every thread an entry or four neighbouring slots, up to two a multiprocessor: every block makes the sums for
+    // itself (1021 sequences, 10^6 slots: 11.2 us with 256 threads twice a multiprocessor, 14 with 512 twice, 15 with 256 once)
+    const long long all = (long long)B + 1 + table_cap + free_cap + (slot_cap + PLAN_PER - 1) / PLAN_PER;
+    const long long want = std::min<long long>((all + PLAN_THREADS - 1) / PLAN_THREADS, 2LL * n_sm);
     SR_CUDA_TRY(launch_dependent(true, page_plan_kernel, dim3((unsigned)std::max<long long>(want, 1)), dim3(PLAN_THREADS), smem,
                                  static_cast<cudaStream_t>(cuda_stream), a));
     return SPECROLL_OK;
