@@ -172,8 +172,9 @@ kv4_load_kernel(const uint8_t *__restrict__ pool, const Kv4Tokens a, uint4 *__re
 #pragma unroll
     for (uint32_t q = 0; q < KV4_EACH; ++q) {
         uint32_t r[4];
-        const uint32_t s = kv4_scale_twice(scale[q]);
-        kv4_word(codes[q], s, kv4_offset(s), r);
+        kv4_word(codes[q], kv4_scale_of(scale[q]), r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = hmul2_bf16(r[i], KV4_UP_PAIR);
         if (c.has(a, q)) __stcs(dst + (unsigned long long)(c.tok + q * a.side) * (a.columns / 2), make_uint4(r[0], r[1], r[2], r[3]));
     }
 }

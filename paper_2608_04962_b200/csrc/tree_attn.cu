@@ -549,16 +549,6 @@ static long long count_chunks(const std::vector<int> &tiles, int ct, int *max_ns
     return n;
 }
 
-static long long count_chunks_of(const int32_t *indptr, int B, int tile_tokens, int ct, int *max_ns) {
-    long long n = 0;
-    for (int b = 0; b < B; ++b) {
-        const int ns = std::max(1, ((indptr[b + 1] - indptr[b] + tile_tokens - 1) / tile_tokens + ct - 1) / ct);
-        n += ns;
-        *max_ns = std::max(*max_ns, ns);
-    }
-    return n;
-}
-
 // Who merges the chunks of a split sequence: the CTA that finishes its last chunk, while the others keep streaming, or
 // (true) a kernel of its own over the whole GPU.  The latter for many chunks (the last CTA would sit on a long chain of
 // dependent loads), and when all work units run side by side, so that nothing streams beside that CTA.
@@ -566,10 +556,10 @@ static bool merge_by_kernel(long long units, int max_ns) { return max_ns >= 5 ||
 
 // Estimated finishing time, in quarter tiles (about a third of a microsecond), of the persistent tcgen05 kernel when
 // sequences of the given tile counts (sorted, longest first) are cut into chunks of at most ct tiles: work units go, in
-// the order the device uses, to whichever of PLAN_SMS CTAs is free first.  A unit costs its K/V tiles, one more for the
+// the order the device uses, to whichever of `places` CTAs is free first.  A unit costs its K/V tiles, one more for the
 // tree tile of a sequence's last chunk, one for the hand-over between units; a chunk of a split sequence adds one
 // for its partial, and the last one the merge when the attention kernel does it, else the merge kernel follows.
-static long long estimate_makespan(const std::vector<int> &tiles, int ct, int copies) {
+static long long estimate_makespan(const std::vector<int> &tiles, int ct, int copies, int places) {
     struct Chunk { int tps, cost; };
     std::vector<Chunk> chunks;
     int max_ns = 1;
@@ -587,7 +577,7 @@ static long long estimate_makespan(const std::vector<int> &tiles, int ct, int co
     }
     std::stable_sort(chunks.begin(), chunks.end(), [](const Chunk &x, const Chunk &y) { return x.tps > y.tps; });
     std::priority_queue<long long, std::vector<long long>, std::greater<long long>> sms;
-    for (int i = 0; i < PLAN_SMS; ++i) sms.push(0);
+    for (int i = 0; i < places; ++i) sms.push(0);
     long long end = 0;
     for (const Chunk &c : chunks)
         for (int k = 0; k < copies; ++k) {
@@ -620,11 +610,13 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     const int TT = p->tile_tokens;
     p->rows = d->N * G;
     p->kv4_few = p->use_tc && kv4 && p->rows <= KV4_FEW_ROWS;
+    int places = PLAN_SMS;  // CTAs that run side by side
     if (p->kv4_few) {
-        // 8 or 16 rows a CTA
+        // 8 or 16 rows a CTA, four or three CTAs on an SM
         p->rows_per_block = p->rows <= 8 ? 8 : 16;
         p->n_rb = (p->rows + p->rows_per_block - 1) / p->rows_per_block;
         p->nodes_per_block = 0;
+        places *= p->rows_per_block == 8 ? 4 : 3;
     } else if (p->use_tc) {
         // row blocks are whole nodes: (node, head-in-group) rows of a block are one TMA box
         // The softmax of a row block costs the same whether the block is full or not, so the rows go into as
@@ -662,28 +654,13 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     // so that the fp32 partials stay a small fraction of the KV bytes.
     const long long ctas_per_tile = (long long)d->Hkv * p->n_rb;
     auto chunk_for = [&](int per_sm_pct) -> int {
-        long long c = (tiles_total * ctas_per_tile * 100 + (long long)PLAN_SMS * per_sm_pct - 1) / ((long long)PLAN_SMS * per_sm_pct);
+        long long c = (tiles_total * ctas_per_tile * 100 + (long long)places * per_sm_pct - 1) / ((long long)places * per_sm_pct);
         if (c < 512 / TT) c = 512 / TT;
         if (c > max_tiles) c = max_tiles > 0 ? max_tiles : 1;
         return (int)c;
     };
     long long ct = chunk_for(p->use_tc ? 100 : 400);
-    if (p->kv4_few && d->B > 0) {
-        // 4-bit cache, few rows: units go to the first free place, in the order of the sequences.  Measured with sequences of equal length
-        // (tenths of a microsecond): a tile takes 6 of an SM's time, a unit beyond its tiles about 12, a unit that runs while others
-        // have ended 9 a tile, the merge 30.
-        long long best = -1;
-        for (int c = 1;; c += (c + 3) / 4) {
-            int ns = 1;
-            const long long units = count_chunks_of(indptr_host, d->B, TT, c, &ns) * ctas_per_tile;
-            const long long m = (tiles_total * ctas_per_tile * 6 + units * 12) / PLAN_SMS + 9 * std::min(c, max_tiles) + (ns > 1 ? 30 + ns : 0);
-            if (best < 0 || m < best) {
-                best = m;
-                ct = c;
-            }
-            if (c >= max_tiles) break;
-        }
-    } else if (p->use_tc && d->B > 0 && tiles_total * ctas_per_tile <= (1LL << 22)) {
+    if (p->use_tc && d->B > 0 && tiles_total * ctas_per_tile <= (1LL << 22)) {
         std::vector<int> tiles((size_t)d->B);
         for (int b = 0; b < d->B; ++b) tiles[(size_t)b] = (indptr_host[b + 1] - indptr_host[b] + TT - 1) / TT;
         std::sort(tiles.begin(), tiles.end(), std::greater<int>());
@@ -694,7 +671,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
             for (int i = 0; i < n_seen; ++i)
                 if (seen[i] == c) return;
             seen[n_seen++] = c;
-            const long long m = estimate_makespan(tiles, c, (int)ctas_per_tile);
+            const long long m = estimate_makespan(tiles, c, (int)ctas_per_tile, places);
             if (best < 0 || m < best) {
                 best = m;
                 ct = c;
@@ -706,7 +683,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
         // merge), and the partials that this adds pass through L2 on an otherwise idle GPU.
         for (int c = 1; c < 512 / TT; ++c) {
             int ns = 1;
-            if (c <= max_tiles && count_chunks(tiles, c, &ns) * ctas_per_tile <= PLAN_SMS) consider(c);
+            if (c <= max_tiles && count_chunks(tiles, c, &ns) * ctas_per_tile <= places) consider(c);
         }
     }
     p->chunk_tiles = (int)ct;

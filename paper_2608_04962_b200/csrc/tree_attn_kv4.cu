@@ -23,7 +23,7 @@ namespace specroll {
 
 namespace akv4 {
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
-constexpr int SLICE = 32, PER_PAGE = SPECROLL_PAGE_TOKENS / SLICE;  // tokens a warp fetches and takes at a time
+constexpr int SLICE = 32;  // tokens a warp fetches and takes at a time
 constexpr int STAGES = 3;
 
 template <int D, int R8>
@@ -196,7 +196,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         // the tokens (of 16) that a thread's indexes stand for: index 2 j + e is token 2 j + (e ^ (j & 1))
         const int k_tok = g ^ ((g >> 1) & 1);               // K rows g and g + 8: tokens k_tok and k_tok + 8
         const int v_a = 2 * c + (c & 1), v_b = v_a ^ 1;     // V pairs: tokens (v_a, v_b) and those + 8
-        const float sc = a.scale_log2;
+        const float sc = a.scale_log2 * KV4_UP;  // (K decodes to 2^-KV4_DOWN of itself; V too, and the tree's probabilities follow it)
         if (tree) {
             const size_t rows_of_b = (size_t)b * N;
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -224,8 +224,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         // Scores (products) of GP groups of 16 tokens to probabilities, in fragments for the product with V.  admits(p, r, e): whether the
         // token of score e (k_tok of group p, + 8 from e = 2 on) counts for row 2 c + (e & 1) of block r; `whole`: they all do.
         // The exponentials are taken against the references as they stand, and a row's sum is the alarm for one that has to move: a
-        // score 2^8 above it makes the sum exceed 2^8.
-        auto softmax = [&](auto &s, bool start, bool whole, auto admits, auto &pf) {
+        // score 2^8 above it makes the sum exceed 2^8.  sc: the scores' factor; down: that of the fragments.
+        auto softmax = [&](auto &s, float sc, float down, bool start, bool whole, auto admits, auto &pf) {
             constexpr int GP = sizeof(s) / sizeof(s[0]);
             float q[GP][R8][4], sum[R8][2];
             auto exps = [&]() {
@@ -292,8 +292,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 l[r][1] += sum[r][1];
 #pragma unroll
                 for (int p = 0; p < GP; ++p) {
-                    pf[p][r][0] = movmatrix(pack_bf16x2(q[p][r][0], q[p][r][1]));
-                    pf[p][r][1] = movmatrix(pack_bf16x2(q[p][r][2], q[p][r][3]));
+                    pf[p][r][0] = movmatrix(pack_bf16x2(q[p][r][0] * down, q[p][r][1] * down));
+                    pf[p][r][1] = movmatrix(pack_bf16x2(q[p][r][2] * down, q[p][r][3] * down));
                 }
             }
         };
@@ -317,7 +317,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             }
             uint32_t pf[1][R8][2];
             const int n0 = 16 * warp + k_tok;
-            softmax(s, true, false, [&](int, int r, int e) {
+            softmax(s, a.scale_log2, 1.0f / KV4_UP, true, false, [&](int, int r, int e) {
                 const int gr = row0 + 8 * r + 2 * c + (e & 1);
                 return gr < a.rows && ((mask.anc[gr / G] >> (n0 + (e & 2 ? 8 : 0))) & 1ull);
             }, pf);
@@ -351,7 +351,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[p][r][e] = 0.f;
                 const int t0 = 16 * p + k_tok;
-                uint32_t kw[2][C::RUN / 8], s2[2], o2[2];
+                uint32_t kw[2][C::RUN / 8];
+                Kv4Scale sk[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const unsigned char *row = tile + (t0 + 8 * h) * Kv4<D>::ROW + (C::RUN / 2) * c;
@@ -363,14 +364,13 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                         kw[h][0] = x.x, kw[h][1] = x.y;
                     }
                     const uint32_t sb = tile[C::CODES + (t0 + 8 * h) * Kv4<D>::SROW + (D == 128 ? c : c >> 1)];
-                    s2[h] = kv4_scale_twice(sb);
-                    o2[h] = kv4_offset(s2[h]);
+                    sk[h] = kv4_scale_of(sb);
                 }
 #pragma unroll
                 for (int j = 0; j < C::RUN / 8; ++j) {
                     uint32_t lo[4], hi[4];
-                    kv4_word(kw[0][j], s2[0], o2[0], lo);
-                    kv4_word(kw[1][j], s2[1], o2[1], hi);
+                    kv4_word(kw[0][j], sk[0], lo);
+                    kv4_word(kw[1][j], sk[1], hi);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t af[4] = {lo[2 * h], hi[2 * h], lo[2 * h + 1], hi[2 * h + 1]};
@@ -382,7 +382,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             // ---- softmax
             uint32_t pf[2][R8][2];
             const int left = L - (first + i * SPECROLL_PAGE_TOKENS) - k_tok;  // > 0: token k_tok is in the sequence
-            softmax(s, i == 0, left + k_tok >= SLICE, [&](int p, int, int e) { return left > 16 * p + (e & 2 ? 8 : 0); }, pf);
+            softmax(s, sc, 1.0f, i == 0, left + k_tok >= SLICE, [&](int p, int, int e) { return left > 16 * p + (e & 2 ? 8 : 0); }, pf);
             // ---- O^T += V^T P^T
             const unsigned char *vt = tile + C::HALF;
 #pragma unroll
@@ -400,16 +400,15 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     }
                     sb[q] = vt[C::CODES + tok * Kv4<D>::SROW + (g * C::VRUN) / 32];
                 }
-                const uint32_t s0 = kv4_scale_pair(sb[0], sb[1]), s1 = kv4_scale_pair(sb[2], sb[3]);
-                const uint32_t f0 = kv4_offset(s0), f1 = kv4_offset(s1);
+                const Kv4Scale s0 = kv4_scale_of(sb[0], sb[1]), s1 = kv4_scale_of(sb[2], sb[3]);
 #pragma unroll
                 for (int j = 0; j < C::VRUN / 8; ++j) {
                     // lower halves: elements 0 2 4 6 of the word, upper halves: 1 3 5 7, of two tokens each
                     uint32_t e0_[4], e1_[4], d0_[4], d1_[4];
-                    kv4_word(__byte_perm(vw[0][j], vw[1][j], 0x5410), s0, f0, e0_);
-                    kv4_word(__byte_perm(vw[0][j], vw[1][j], 0x7632), s0, f0, d0_);
-                    kv4_word(__byte_perm(vw[2][j], vw[3][j], 0x5410), s1, f1, e1_);
-                    kv4_word(__byte_perm(vw[2][j], vw[3][j], 0x7632), s1, f1, d1_);
+                    kv4_word(__byte_perm(vw[0][j], vw[1][j], 0x5410), s0, e0_);
+                    kv4_word(__byte_perm(vw[0][j], vw[1][j], 0x7632), s0, d0_);
+                    kv4_word(__byte_perm(vw[2][j], vw[3][j], 0x5410), s1, e1_);
+                    kv4_word(__byte_perm(vw[2][j], vw[3][j], 0x7632), s1, d1_);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const uint32_t af[4] = {e0_[q], d0_[q], e1_[q], d1_[q]};
@@ -484,6 +483,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             acc.z += f * x.z;
             acc.w += f * x.w;
         }
+        acc = make_float4(acc.x * KV4_UP, acc.y * KV4_UP, acc.z * KV4_UP, acc.w * KV4_UP);
         const int n = gr / G, gq = gr % G;
         if (n_splits == 1) {
             const float inv = sum > 0.f ? 1.0f / sum : 0.f;

@@ -42,6 +42,9 @@
 // kernel) the loading thread fetches its first cache tiles before the wait that precedes every other access.
 #include <math.h>
 
+#include <algorithm>
+#include <atomic>
+
 #include "kv4.cuh"
 #include "tc05.cuh"
 #include "tree_attn.cuh"
@@ -78,8 +81,9 @@ struct Cfg {
     static constexpr int THREADS = 32 * (DECODE0 + DECODE_TEAMS * DECODE_WARPS);
     // Registers a thread of each role, where there is decoding: 768 threads get 80 each at the launch, and the groups of four warps share
     // the same sum out anew (the softmax threads keep a tile's probabilities in registers).
-    static constexpr int REGS_LOAD = 80, REGS_SOFT = 112, REGS_OUT = 80, REGS_DECODE = 48;
-    static_assert(!KV4 || REGS_LOAD + REGS_SOFT * (SOFTMAX_THREADS / 128) + REGS_OUT + REGS_DECODE * DECODE_TEAMS == 80 * (THREADS / 128),
+    static constexpr int REGS_LOAD = 72, REGS_SOFT = 112, REGS_OUT = 88, REGS_DECODE = 48;
+    static constexpr int REGS = 65536 / THREADS / 8 * 8;  // a thread's at the launch
+    static_assert(!KV4 || (REGS_LOAD + REGS_SOFT * (SOFTMAX_THREADS / 128) + REGS_OUT + REGS_DECODE * DECODE_TEAMS) * 128 <= REGS * THREADS,
                   "no more registers than the launch gave");
     static constexpr int FULL_ARRIVALS = KV4 ? DECODE_WARPS : 1;  // of a ring stage: the decoding warps, or the loading thread
     static constexpr int Q_BYTES = NBOX * BOX_BYTES;   // the Q block of one unit
@@ -138,6 +142,13 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+
+// This warp's registers a thread from `LAUNCH` to TO (decreasing to more, or increasing to fewer, is an illegal instruction).
+template <int TO, int LAUNCH>
+__device__ __forceinline__ void set_registers() {
+    if constexpr (TO > LAUNCH) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TO));
+    else if constexpr (TO < LAUNCH) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TO));
 }
 
 __device__ __forceinline__ unsigned short bf16_bits_rn(float x) {
@@ -261,11 +272,11 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     }
 
-    if constexpr (KV4) {  // (whole groups of four warps; those that give come first, those that take wait for them)
-        if (warp < C::SOFT0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_LOAD));
-        else if (warp < C::OUT0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS_SOFT));
-        else if (warp >= C::DECODE0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_DECODE));
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_OUT));
+    if constexpr (KV4) {  // (whole groups of four warps; those that take registers wait until the others have given theirs)
+        if (warp < C::SOFT0) set_registers<C::REGS_LOAD, C::REGS>();
+        else if (warp < C::OUT0) set_registers<C::REGS_SOFT, C::REGS>();
+        else if (warp < C::DECODE0) set_registers<C::REGS_OUT, C::REGS>();
+        else set_registers<C::REGS_DECODE, C::REGS>();
     }
 
     // Sums the partials of all chunks of one (sequence, kv head, row block) for columns [col0, col0 + ncols) of one row;
@@ -732,7 +743,6 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     continue;
                 }
                 const unsigned char *codes = aligned + QS * C::Q_BYTES + RS * C::KV_BYTES + s * C::SLOT_BYTES;
-                const uint32_t keep = kind == CODES ? 0xffffffffu : 0u;  // (no such page: zeros)
                 // (all loads ahead of the first store: the compiler may not move them across one)
                 constexpr int STEPS = BN / (C::DECODE_WARPS * STEP), TOKENS = C::DECODE_WARPS * STEP;
                 uint4 w[STEPS];
@@ -740,18 +750,19 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
                 for (int it = 0; it < STEPS; ++it) {
                     w[it] = *reinterpret_cast<const uint4 *>(codes + code0 + it * TOKENS * Kv4<D>::ROW);
+                    if (kind != CODES) w[it] = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);  // (no such page: zeros)
                     sb[it] = codes[scale0 + it * TOKENS * Kv4<D>::SROW];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) dst[i] = stage_addr(st) + off[i];
 #pragma unroll
                 for (int it = 0; it < STEPS; ++it) {
-                    const uint32_t s2 = kv4_scale_twice(sb[it]) & keep, o2 = kv4_offset(s2);
+                    const Kv4Scale sc = kv4_scale_of(sb[it]);
                     const uint32_t ww[4] = {w[it].x, w[it].y, w[it].z, w[it].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint32_t r[4];
-                        kv4_word(ww[i], s2, o2, r);
+                        kv4_word(ww[i], sc, r);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst[i] + (uint32_t)(it * TOKENS * 128)), "r"(r[0]),
                                      "r"(r[1]), "r"(r[2]), "r"(r[3])
                                      : "memory");
@@ -816,7 +827,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const uint32_t o_t = t_lane + C::O_COL;
             const int n = row_ok ? gr / G : 0, g = row_ok ? gr % G : 0;
             const bool direct = (n_splits == 1);
-            const float inv = direct ? (lt > 0.f ? 1.0f / lt : 0.f) : 1.0f;
+            const float inv = (direct ? (lt > 0.f ? 1.0f / lt : 0.f) : 1.0f) * (KV4 ? KV4_UP : 1.0f);
             __nv_bfloat16 *dst_o = a.O + (((size_t)b * N + n) * a.Hq + hkv * G + g) * D;
             // partials are stored [unit][float4 column][row] so that a warp's stores are contiguous
             const size_t pbase = ((size_t)item * a.Hkv + hkv) * (size_t)(D / 4) * a.rows_pad;
@@ -850,8 +861,10 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
                     for (int i2 = 0; i2 < 32; i2 += 4)
                         dst_p[(size_t)((c + i2) / 4) * a.rows_pad] =
-                            make_float4(__uint_as_float(o[i2]), __uint_as_float(o[i2 + 1]), __uint_as_float(o[i2 + 2]),
-                                        __uint_as_float(o[i2 + 3]));
+                            KV4 ? make_float4(__uint_as_float(o[i2]) * inv, __uint_as_float(o[i2 + 1]) * inv, __uint_as_float(o[i2 + 2]) * inv,
+                                              __uint_as_float(o[i2 + 3]) * inv)
+                                : make_float4(__uint_as_float(o[i2]), __uint_as_float(o[i2 + 1]), __uint_as_float(o[i2 + 2]),
+                                              __uint_as_float(o[i2 + 3]));
                 }
             }
             const size_t prow = ((size_t)item * a.Hkv + hkv) * a.rows_pad + (row_ok ? gr : 0);
@@ -892,9 +905,11 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const int team = ws >> 2;
             const int lg = warp & 3;  // TMEM lane group of this warp
             const int row = lg * 32 + lane;
+            // (pages decode to 2^-KV4_DOWN of their values, K and V; the tree's tile does not: its scores take the factor back and its
+            // probabilities follow V's)
+            const float sc = KV4 ? a.scale_log2 * KV4_UP : a.scale_log2;
             const uint32_t t_lane = tmem_base + ((uint32_t)(lg * 32) << 16);
             const uint32_t o_t = t_lane + C::O_COL;
-            const float sc = a.scale_log2;
             volatile float *mref = reinterpret_cast<volatile float *>(xch_base);  // [2 slots][128 rows]
             uint32_t gt = 0;  // tiles so far (all units, both teams)
             bool ok = true;
@@ -956,14 +971,15 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                             }
                             unpack_f32x2(add_f32x2(ls2, ls3), ls0, ls1);
                         } else {
+                            const float down = KV4 && tree ? 1.0f / KV4_UP : 1.0f, sct = sc * down;
 #pragma unroll
                             for (int i2 = 0; i2 < 32; i2 += 2) {
                                 const bool b0 = (bc >> i2) & 1u, b1 = (bc >> (i2 + 1)) & 1u;
-                                const float p0 = b0 ? ex2_approx(fmaf(__uint_as_float(src[i2]), sc, -mref_)) : 0.f;
-                                const float p1 = b1 ? ex2_approx(fmaf(__uint_as_float(src[i2 + 1]), sc, -mref_)) : 0.f;
+                                const float p0 = b0 ? ex2_approx(fmaf(__uint_as_float(src[i2]), sct, -mref_)) : 0.f;
+                                const float p1 = b1 ? ex2_approx(fmaf(__uint_as_float(src[i2 + 1]), sct, -mref_)) : 0.f;
                                 ls0 += p0;
                                 ls1 += p1;
-                                pk[i2 >> 1] = pack_bf16x2(p0, p1);
+                                pk[i2 >> 1] = KV4 ? pack_bf16x2(p0 * down, p1 * down) : pack_bf16x2(p0, p1);
                             }
                         }
                     };
@@ -1030,7 +1046,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                                     if ((bc >> i2) & 1u) mx0 = fmaxf(mx0, __uint_as_float(x[i2]));
                             }
                         }
-                        const float mt = fmaxf(mx0, mx1) * sc;
+                        const float mt = fmaxf(mx0, mx1) * (KV4 && tree ? a.scale_log2 : sc);
                         // ... then the reference: the other team's after the tile before (this thread's share of the sum
                         // moves with it), raised if this tile's maximum is more than 2^8 above it
                         ok = predecessor();
@@ -1379,6 +1395,17 @@ static int launch_tc(const AttnArgs &a, const TopoMask &mask, long long T_kv, in
     const unsigned grid = (unsigned)(a.total_work < ctas ? a.total_work : ctas);
     auto *const kern = a.total_work <= (int)grid && a.merge_mode != 0 ? tree_attn_tc_kernel<D, TEAMS, true, KV4> : tree_attn_tc_kernel<D, TEAMS, false, KV4>;
     if ((rc = device_setup(reinterpret_cast<const void *>(kern), C::SMEM, nullptr)) != SPECROLL_OK) return rc;
+    if constexpr (KV4) {
+        // the roles share out REGS registers a thread: a kernel compiled to fewer would wait for registers that it was not given
+        static std::atomic<int> fewest{0};
+        if (fewest.load(std::memory_order_relaxed) == 0) {
+            cudaFuncAttributes one = {}, many = {};
+            SR_CUDA_TRY(cudaFuncGetAttributes(&one, tree_attn_tc_kernel<D, TEAMS, true, true>));
+            SR_CUDA_TRY(cudaFuncGetAttributes(&many, tree_attn_tc_kernel<D, TEAMS, false, true>));
+            fewest.store(std::min(one.numRegs, many.numRegs), std::memory_order_relaxed);
+        }
+        if (fewest.load(std::memory_order_relaxed) < C::REGS) return note_cuda_error(cudaErrorLaunchOutOfResources);
+    }
     // Programmatic stream serialization: the CTAs may be set up (barriers, tensor memory, zeroed Q buffers) while
     // the kernel before this one in the stream is still running its last CTAs; the kernel itself waits for
     // that kernel's completion before it reads anything (griddepcontrol.wait).
