@@ -612,11 +612,11 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     p->kv4_few = p->use_tc && kv4 && p->rows <= KV4_FEW_ROWS;
     int places = PLAN_SMS;  // CTAs that run side by side
     if (p->kv4_few) {
-        // 8 or 16 rows a CTA, four or three CTAs on an SM
+        // 8 or 16 rows a CTA
         p->rows_per_block = p->rows <= 8 ? 8 : 16;
         p->n_rb = (p->rows + p->rows_per_block - 1) / p->rows_per_block;
         p->nodes_per_block = 0;
-        places *= p->rows_per_block == 8 ? 4 : 3;
+        places *= p->rows_per_block == 8 ? KV4_CTAS_8 : KV4_CTAS_16;
     } else if (p->use_tc) {
         // row blocks are whole nodes: (node, head-in-group) rows of a block are one TMA box
         // The softmax of a row block costs the same whether the block is full or not, so the rows go into as
@@ -880,7 +880,7 @@ static int run_tree_attn(const specroll_attn_desc *d, const void *Q, const void 
     if (p.use_tc) {
         const int rc = p.kv4_few ? launch_attn_kv4(a, mask, d->D, status, st) : launch_attn_tc(a, mask, d->D, T_kv, status, st);
         if (rc != SPECROLL_OK || p.merge_mode != 2 || p.items <= d->B) return rc;
-        if (p.kv4_few) return launch_attn_merge_kv4(a, d->D, st);
+        if (p.kv4_few) return launch_attn_merge_kv4(a, d->D, p.max_splits, st);
         return launch_attn_merge_tc(a, d->D, p.items, p.max_splits, st);
     }
     if (d->D == 128) return launch_attn<128>(a, mask, p, d->Hkv, n_out, st);

@@ -44,8 +44,10 @@ constexpr int ATTN_HAND_CTAS = 256;  // CTAs the hand-over area is sized for (th
 // tcgen05 kernel (tree_attn_tc.cu).  T_kv = total cached tokens.  Launches the main kernel only.
 int launch_attn_tc(const AttnArgs &a, const TopoMask &mask, int D, long long T_kv, int32_t *status, cudaStream_t st);
 // Kernel for a 4-bit cache and few query rows per KV head (tree_attn_kv4.cu); the same plan and partials.
+// CTAs of it that run side by side on an SM, with 8 and with 16 query rows: what registers and shared memory have room for.
+constexpr int KV4_CTAS_8 = 4, KV4_CTAS_16 = 3;
 int launch_attn_kv4(const AttnArgs &a, const TopoMask &mask, int D, int32_t *status, cudaStream_t st);
-int launch_attn_merge_kv4(const AttnArgs &a, int D, cudaStream_t st);  // merges the chunks of split sequences after it
+int launch_attn_merge_kv4(const AttnArgs &a, int D, int max_splits, cudaStream_t st);  // merges the chunks of split sequences after it
 // Merges the chunks of split sequences after launch_attn_tc when a.merge_mode == 2.  items = chunks in the plan, max_splits = those of
 // the longest sequence.
 int launch_attn_merge_tc(const AttnArgs &a, int D, int items, int max_splits, cudaStream_t st);

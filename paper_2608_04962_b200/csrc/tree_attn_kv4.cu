@@ -39,7 +39,7 @@ struct Cfg {
     static constexpr int JOIN = WARPS * (O_FLOATS + 2 * ROWS) * 4;
     static constexpr int BODY = (RING > JOIN ? RING : JOIN);
     static constexpr int SMEM = BODY + 8 * WARPS * STAGES + 16;
-    static constexpr int CTAS = R8 == 1 ? 4 : 3;  // side by side on an SM: what registers and shared memory have room for
+    static constexpr int CTAS = R8 == 1 ? KV4_CTAS_8 : KV4_CTAS_16;
     static_assert(SCALES % 16 == 0 && CTAS * (SMEM + 1024) <= 233472, "bulk copies; shared memory of an SM");
 };
 
@@ -73,7 +73,11 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     // lengths (a plan made by a kernel in front took ten microseconds for 256 sequences).
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;  // (seconds ahead of any wait that could run out)
     const int rb = (int)blockIdx.x % a.n_rb, hkv = (int)blockIdx.x / a.n_rb % a.Hkv, item = (int)blockIdx.x / a.n_rb / a.Hkv;
-    {
+    int b = item, split = 0, n_splits = 1, L, slot0;
+    if (a.items == a.B) {  // (nothing is cut)
+        L = max(__ldg(a.kv_len + b), 0);
+        slot0 = __ldg(a.page_indptr + b);
+    } else {
         volatile int *const found = reinterpret_cast<volatile int *>(smem);  // [0..5]: the unit, [8 ..]: chunks of the warps' sequences
         const int per = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
         auto chunks = [&](int len) { return max(1, ((len + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS + a.chunk_tiles - 1) / a.chunk_tiles); };
@@ -118,19 +122,24 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             }
         }
         __syncthreads();
+        b = found[0];
+        split = found[1];
+        n_splits = found[2];
+        L = found[3];
+        slot0 = found[4];
+        __syncthreads();
+        if (b < 0) return;  // (lengths that make fewer chunks than the host's)
     }
-    const volatile int *const unit_s = reinterpret_cast<const volatile int *>(smem);
-    const int b = unit_s[0], split = unit_s[1], n_splits = unit_s[2], L = unit_s[3], slot0 = unit_s[4];
-    __syncthreads();
-    if (b < 0) return;  // (lengths that make fewer chunks than the host's)
     const int tiles_b = (L + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS;
     const int tps = (tiles_b + n_splits - 1) / n_splits;
     const int t_lo = min(tiles_b, split * tps), n_t = min(tiles_b, t_lo + tps) - t_lo;
     const bool has_tree = split == n_splits - 1;
     const int N = a.N, G = a.G, row0 = rb * C::ROWS;
-    // this warp's slices: slice i is tokens first + 128 i .. + 32 of the sequence, a quarter of a page
+    // this warp's slices: slice i is the 32 tokens of the sequence from first + STRIDE i on, a quarter of a page
+    constexpr int STRIDE = WARPS * SLICE;
     const int first = t_lo * SPECROLL_PAGE_TOKENS + warp * SLICE, end = min(L, (t_lo + n_t) * SPECROLL_PAGE_TOKENS);
-    const int n_i = end > first ? (end - first + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS : 0;
+    const int n_i = end > first ? (end - first + STRIDE - 1) / STRIDE : 0;
+    auto page_at = [&](int i) { return (warp * SLICE + STRIDE * i) / SPECROLL_PAGE_TOKENS; };
 
     float o[R8][C::MB][4];
     float m[R8][2], ref[R8][2], l[R8][2];  // reference maxima (ref: the same, but 0 where there is none yet) and sums
@@ -153,8 +162,9 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         if (page >= 0 && page < a.n_pages) {
             if (lane == 0) {
                 const uint32_t dst = smem_u32(mine) + s * C::BYTES;
-                const uint8_t *k = a.pool + ((size_t)page * a.Hkv + hkv) * (2 * Kv4<D>::TILE) + warp * C::CODES;
-                const uint8_t *ks = k + Kv4<D>::CODES - warp * (C::CODES - C::SCALES);
+                const int part = (warp + WARPS * i) % (SPECROLL_PAGE_TOKENS / SLICE);
+                const uint8_t *k = a.pool + ((size_t)page * a.Hkv + hkv) * (2 * Kv4<D>::TILE) + part * C::CODES;
+                const uint8_t *ks = k + Kv4<D>::CODES - part * (C::CODES - C::SCALES);
                 mbar_arrive_expect_tx(bar, C::BYTES);
                 bulk_load(dst, k, C::CODES, bar);
                 bulk_load(dst + C::CODES, ks, C::SCALES, bar);
@@ -169,7 +179,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     };
     int page[STAGES + 1];
 #pragma unroll
-    for (int i = 0; i <= STAGES; ++i) page[i] = i < n_i ? __ldg(pt + i) : -1;
+    for (int i = 0; i <= STAGES; ++i) page[i] = i < n_i ? __ldg(pt + page_at(i)) : -1;
 
     {
         // ------------------------------------------------------------------ attention
@@ -381,7 +391,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             }
             // ---- softmax
             uint32_t pf[2][R8][2];
-            const int left = L - (first + i * SPECROLL_PAGE_TOKENS) - k_tok;  // > 0: token k_tok is in the sequence
+            const int left = L - (first + i * STRIDE) - k_tok;  // > 0: token k_tok is in the sequence
             softmax(s, sc, 1.0f, i == 0, left + k_tok >= SLICE, [&](int p, int, int e) { return left > 16 * p + (e & 2 ? 8 : 0); }, pf);
             // ---- O^T += V^T P^T
             const unsigned char *vt = tile + C::HALF;
@@ -420,7 +430,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             __syncwarp();
             if (i + STAGES < n_i) {
                 load(i + STAGES, next_page);
-                next_page = i + STAGES + 1 < n_i ? __ldg(pt + i + STAGES + 1) : 0;
+                next_page = i + STAGES + 1 < n_i ? __ldg(pt + page_at(i + STAGES + 1)) : 0;
             }
         }
 #pragma unroll
@@ -509,13 +519,13 @@ static int launch_kv4(const AttnArgs &a, const TopoMask &mask, int32_t *status, 
     return SPECROLL_OK;
 }
 
-// Sums the chunks of every split sequence.  grid = (B, Hkv, 4): a block has a quarter of D of all rows of one (sequence, KV head), 4 D floats
-// of which a thread takes four, and as many parts of the chunks as 256 threads have room for; a part's chunks are taken eight at a
-// time with all their loads in flight.  Launched as a programmatic dependent of the attention kernel, which
-// lets it start only behind its own wait: the lengths can be read ahead of the wait for the partials.
-template <int D, int ROWS>
+// Sums the chunks of every split sequence.  grid = (B, Hkv, Z): a block has a Z-th of D of all rows of one (sequence, KV head), four floats
+// a thread, and as many parts of the chunks as 256 threads have room for; a part's chunks are taken eight at a time with all their loads
+// in flight.  Z = 4 where some sequence has more chunks than that, else the fewest blocks.  Launched as a programmatic dependent of the
+// attention kernel, which lets it start only behind its own wait: the lengths can be read ahead of the wait for the partials.
+template <int D, int ROWS, int Z>
 __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
-    constexpr int COLS = D / 16, ITEMS = ROWS * COLS, PARTS = 256 / ITEMS, STEP = 8;
+    constexpr int COLS = D / 4 / Z, ITEMS = ROWS * COLS, PARTS = 256 / ITEMS, STEP = 8;
     static_assert(PARTS >= 1 && PARTS * ITEMS == 256, "whole blocks");
     __shared__ float2 sh_ml[256];
     __shared__ float4 sh_acc[256];
@@ -590,12 +600,18 @@ __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     }
 }
 
-int launch_attn_merge_kv4(const AttnArgs &a, int D, cudaStream_t st) {
-    const bool one = a.rows_per_block == 8;
-    auto *const kern = D == 128 ? (one ? attn_merge_kv4_kernel<128, 8> : attn_merge_kv4_kernel<128, 16>)
-                                : (one ? attn_merge_kv4_kernel<64, 8> : attn_merge_kv4_kernel<64, 16>);
-    SR_CUDA_TRY(launch_dependent(!a.no_pdl, kern, dim3((unsigned)a.B, (unsigned)a.Hkv, 4), dim3(256), 0, st, a));
+template <int D, int ROWS, int Z>
+static int launch_merge(const AttnArgs &a, cudaStream_t st) {
+    SR_CUDA_TRY(launch_dependent(!a.no_pdl, attn_merge_kv4_kernel<D, ROWS, Z>, dim3((unsigned)a.B, (unsigned)a.Hkv, Z), dim3(256), 0, st, a));
     return SPECROLL_OK;
+}
+
+int launch_attn_merge_kv4(const AttnArgs &a, int D, int max_splits, cudaStream_t st) {
+    const bool one = a.rows_per_block == 8, few = max_splits <= 8;
+    if (D == 128 && one) return few ? launch_merge<128, 8, 1>(a, st) : launch_merge<128, 8, 4>(a, st);
+    if (D == 128) return few ? launch_merge<128, 16, 2>(a, st) : launch_merge<128, 16, 4>(a, st);
+    if (one) return few ? launch_merge<64, 8, 1>(a, st) : launch_merge<64, 8, 4>(a, st);
+    return few ? launch_merge<64, 16, 1>(a, st) : launch_merge<64, 16, 4>(a, st);
 }
 
 int launch_attn_kv4(const AttnArgs &a, const TopoMask &mask, int D, int32_t *status, cudaStream_t st) {
