@@ -69,10 +69,11 @@ struct Cfg {
     // three tiles ahead of P V), so every load has the whole ring's depth to land; separate rings would need
     // three stages each for that, which does not fit beside two Q buffers.
     static constexpr int RS = KV4 ? 4 : 5;   // ring stages
-    // 4-bit cache: K and V of a page arrive as codes in SS staging slots; four warps decode them into the ring's stages
-    static constexpr int SS = KV4 ? 3 : 0, SLOT_BYTES = KV4 ? Kv4<D>::TILE : 0, DECODE_WARPS = KV4 ? 4 : 0, DECODE_TEAMS = KV4 ? 2 : 0;
+    // 4-bit cache: K and V of a page arrive as codes in SS staging slots; two teams of four warps decode them into the ring's stages
+    static constexpr int SS = KV4 ? 3 : 0, SLOT_BYTES = KV4 ? Kv4<D>::TILE : 0, DECODE_WARPS = KV4 ? 4 : 0, DECODE_TEAMS = 2;
     // Job n is in slot n mod SS and is told on barrier n mod SF, which only one team waits for: it has then seen every phase before.
     static constexpr int SF = SS * DECODE_TEAMS;
+    static_assert(!KV4 || (RS % DECODE_TEAMS == 0 && SF % DECODE_TEAMS == 0), "a stage's and a barrier's jobs are one team's");
     static constexpr int QS = 2;   // Q buffers (units)
     static constexpr int MMA_WARPS = 2;  // issuing threads (one lane of each)
     static constexpr int SOFTMAX_THREADS = 256, OUT_THREADS = 128;
@@ -162,11 +163,13 @@ __device__ __forceinline__ float bf16_bits_to_float(unsigned short b) { return _
 // asked at run time it cost the shapes with many units 1-4 %.)
 // KV4: the cache is a 4-bit paged pool (tmK and tmV are not used).  Pages come as codes into staging slots by untiled bulk copies; two
 // teams of four warps take the slots in turn and decode them into the ring's stages, in the 128-byte swizzle that TMA would have left.
-// The tree's tiles go through the same queue, as a slot that names the tile, and are fetched into their stages from there, so that
-// stages are filled by the decoding teams alone.  A wait on a barrier's parity is right while the waiter is at most one phase behind or
-// ahead: a stage's job waits for the stage's use before to be consumed, so that use's own job must not be still waiting for the
-// one before it.  With SS = 3 slots only two neighbouring jobs of the queue can be in the teams' hands at a time (the one after them needs a slot that
-// the first still holds), and neighbours' positions are one or three apart, never the RS = 4 of two uses of one stage.
+// The tree's tiles go through the same queue, as a slot that names the tile, and are fetched into their stages from there: job n of the
+// queue fills ring position n.  A wait for a barrier's parity is right only while the waiter is at most one phase away, and it is: the
+// stages are a multiple of the teams, so that all jobs of a stage are one team's, one after the other; and a slot's filling is told on one of
+// SF barriers, a multiple of the teams too (copies land in any order: on one barrier a slot, with an odd number of slots, a team
+// would have to tell two phases apart that it had not both seen).  What bounds it: 1.15 us a tile, where the tensor operations need 0.55, the
+// exponentials as much and shared memory 0.8 (codes in, 64 KB of decoded tiles in and out, Q); without decoding 0.95, without
+// decoding and exponentials 0.8.  One team of eight warps: 0.1 us a tile more, one of four 0.25.
 template <int D, bool TEAMS, bool ONE, bool KV4>
 __global__ void __launch_bounds__(attc::Cfg<D, TEAMS, KV4>::THREADS, 1)
 tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,

@@ -411,3 +411,152 @@ def test_two_streams_with_workspaces_of_their_own():
                 got[i].append(_run(xs[i]))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want[i]) for i in range(2) for o in got[i])
+
+
+@pytest.mark.parametrize("N,Hq", [(1, 8), (24, 12)])
+def test_places_beyond_four_gigabytes(N, Hq):
+    """A pool of 5 GB of which a few pages near its end and its beginning are used."""
+    g = np.random.default_rng(17)
+    Hkv, D, lens = 2, 128, np.array([300, 129], np.int32)
+    n_pages = 5 * (1 << 30) // (Hkv * 2 * S.kv4_tile_bytes(D))
+    pool = torch.empty(n_pages, Hkv, 2, S.kv4_tile_bytes(D), dtype=torch.uint8, device="cuda")
+    table, indptr = np.array([n_pages - 1, 0, n_pages - 2, n_pages // 2, n_pages - 7], np.int32), np.array([0, 3, 5], np.int32)
+    slots = np.concatenate([table[indptr[b] + np.arange(lens[b]) // 128].astype(np.int64) * 128 + np.arange(lens[b]) % 128 for b in range(2)])
+    K, V = _bits(g, len(slots), Hkv, D), _bits(g, len(slots), Hkv, D)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    S.kv4_store(dev_bf16(K), dev_bf16(V), dev(slots), pool, status=status)
+    vals = [ref.kv4_values(*ref.kv4_quantise(_f64(x))) for x in (K, V)]
+    for got, want in zip(S.kv4_load(pool, dev(slots), status=status), vals):
+        assert np.array_equal(host(got.double()), want)
+    parent = np.array([-1] + [int(g.integers(0, n)) for n in range(1, N)], np.int32)
+    Q, Kt, Vt = _bits(g, 2, N, Hq, D), _bits(g, 2, N, Hkv, D), _bits(g, 2, N, Hkv, D)
+    want, wl, A, dot = ref.tree_attn64(_f64(Q), *[np.split(x, [300]) for x in vals], lens, _f64(Kt), _f64(Vt), parent, D ** -0.5)
+    O = S.tree_attn_kv4(dev_bf16(Q), pool, dev(table), dev(indptr), dev(lens), lens, dev_bf16(Kt), dev_bf16(Vt), parent, check_status=True)
+    assert (np.abs(host(O.double()) - want) <= 2.0 ** -8 * (A + np.abs(want)) + 2 * (D * 2.0 ** -23 * dot + 2.0 ** -18) * A).all()
+    path, n_acc = np.zeros((2, 2), np.int32), np.zeros(2, np.int32)          # the first node's rows behind the last token
+    S.commit_path_kv4(dev_bf16(Kt), dev_bf16(Vt), dev(path), dev(n_acc), pool, dev(table), dev(indptr), dev(lens), status=status)
+    at = np.array([table[2] * 128 + 300 % 128, table[4] * 128 + 129 % 128], np.int64)
+    k, _ = S.kv4_load(pool, dev(at))
+    assert np.array_equal(host(k.double()), ref.kv4_values(*ref.kv4_quantise(_f64(Kt[:, 0])))) and int(status) == 0
+
+
+@pytest.mark.parametrize("N,Hq", [(1, 8), (24, 12)])
+def test_a_round_in_one_graph(N, Hq):
+    """Pages, attention and commit captured together and replayed on other lengths' caches of the same plan."""
+    x, y = (_case(4, N, Hq, 2, 128, [300, 130, 128, 1], seed=s, spare=5) for s in (18, 19))
+    bf = ("Q", "Kt", "Vt")
+    t = {k: (dev_bf16 if k in bf else dev)(x[k]) for k in ("Q", "pool", "table", "indptr", "len", "Kt", "Vt")}
+    n_pages = x["pool"].shape[0]
+    free = np.setdiff1d(np.arange(n_pages), x["table"]).astype(np.int32)
+    t |= {"free": dev(np.concatenate([free, np.zeros(n_pages - len(free), np.int32)])), "n_free": dev(np.array([len(free)], np.int32)),
+          "add": torch.full((4,), 2, dtype=torch.int32, device="cuda"), "path": dev(np.tile(np.array([0, N - 1], np.int32), (4, 1))),
+          "n_acc": dev(np.array([1, 0, 1, 0], np.int32))}
+    out = {}
+
+    def round_():
+        out["plan"] = S.page_plan(t["len"], t["add"], t["table"], t["indptr"], t["free"], t["n_free"], n_pages, 8)
+        out["O"] = S.tree_attn_kv4(t["Q"], t["pool"], out["plan"]["page_table"], out["plan"]["page_indptr"], t["len"], x["len"], t["Kt"], t["Vt"],
+                                   x["parent"])
+        out["len"] = torch.empty_like(t["len"])
+        S.commit_path_kv4(t["Kt"], t["Vt"], t["path"], t["n_acc"], t["pool"], out["plan"]["page_table"], out["plan"]["page_indptr"], t["len"],
+                          kv_len_out=out["len"])
+        out["KV"] = S.kv4_load(t["pool"], out["plan"]["slot_map"])
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        round_()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        round_()
+    for k in ("Q", "pool", "Kt", "Vt", "table"):
+        t[k].copy_((dev_bf16 if k in bf else dev)(y[k]))
+    free = np.setdiff1d(np.arange(n_pages), y["table"]).astype(np.int32)
+    t["free"][:len(free)] = dev(free)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = _run({**y, "parent": x["parent"]})
+    assert torch.equal(out["O"], want) and host(out["len"]).tolist() == [302, 131, 130, 2]
+    rows = ref.kv4_values(*ref.kv4_quantise(np.stack([_f64(y["Kt"])[:, 0], _f64(y["Kt"])[:, N - 1]], 1)))
+    got = host(out["KV"][0].double()).reshape(4, 2, 2, 128)
+    for b, n in enumerate((2, 1, 2, 1)):
+        assert np.array_equal(got[b, :n], rows[b, :n])
+
+
+def test_a_settled_cache_written_two_kernels_ago():
+    """Commit into layer B's pool, attention of layer A, attention of layer B, which may fetch its pages while A's is finishing."""
+    x = _case(8, 16, 12, 2, 128, [700, 64, 1500, 333, 129, 2900, 256, 77], seed=21, spare=8)
+    t = {k: (dev_bf16 if k in ("Q", "Kt", "Vt") else dev)(x[k]) for k in ("Q", "pool", "table", "indptr", "len", "Kt", "Vt")}
+    path, n_acc, first = torch.arange(5, dtype=torch.int32, device="cuda").repeat(8, 1), torch.full((8,), 4, dtype=torch.int32, device="cuda"), torch.zeros_like(t["len"])
+    A, B = t["pool"], t["pool"].clone()
+    others = [torch.zeros_like(B) for _ in range(12)]
+    ws = S.alloc(S.tree_attn_kv4_workspace_bytes(8, 16, 12, 2, 128, x["len"]), dtype=torch.uint8, device="cuda")
+
+    def attn(pool, flags):
+        return S.tree_attn_kv4(t["Q"], pool, t["table"], t["indptr"], t["len"], x["len"], t["Kt"], t["Vt"], x["parent"], workspace=ws, flags=flags)
+
+    def commit(pools):
+        S.commit_path_kv4_layers([t["Kt"]] * len(pools), [t["Vt"]] * len(pools), path, n_acc, pools, t["table"], t["indptr"], first)
+    commit([B])
+    want_a, want_b = attn(A, 0), attn(B, 0)
+    assert not torch.equal(want_a, want_b)
+    for _ in range(20):
+        B.copy_(A)
+        torch.cuda.synchronize()
+        commit(others + [B])
+        flags = S.ATTN_REUSE_PLAN | S.ATTN_CACHE_SETTLED
+        got_a, got_b = attn(A, flags), attn(B, flags)
+        torch.cuda.synchronize()
+        assert torch.equal(got_a, want_a) and torch.equal(got_b, want_b)
+    assert S.workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("N,Hq", [(1, 3), (6, 3)])
+def test_4096_sequences_and_no_more(N, Hq):
+    B, D = 4096, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    lens = np.random.default_rng(1).integers(0, 130, B).astype(np.int32)
+    pages = 64
+    pool = torch.randint(0, 255, (pages, 1, 2, S.kv4_tile_bytes(D)), dtype=torch.uint8, device="cuda", generator=g)
+    pool[..., 64 * D:] = 8 * 20                                              # (scales of one)
+    table = torch.randint(0, pages, (2 * B,), dtype=torch.int32, device="cuda", generator=g)
+    indptr = torch.arange(0, 2 * B + 1, 2, dtype=torch.int32, device="cuda")
+    Q, Kt, Vt = (torch.randn(B, N, h, D, device="cuda", generator=g).bfloat16() for h in (Hq, 1, 1))
+    parent = np.arange(-1, N - 1, dtype=np.int32)
+
+    def call(n):
+        return S.tree_attn_kv4(Q[:n].contiguous(), pool, table, indptr[:n + 1].contiguous(), dev(lens[:n]), lens[:n], Kt[:n].contiguous(),
+                               Vt[:n].contiguous(), parent)
+    O = call(B)
+    for b in (0, 1, 777, 2048, 4095):                                        # (each like the call of it alone)
+        one = S.tree_attn_kv4(Q[b:b + 1].contiguous(), pool, table[2 * b:2 * b + 2].contiguous(), indptr[:2].contiguous(), dev(lens[b:b + 1]),
+                              lens[b:b + 1], Kt[b:b + 1].contiguous(), Vt[b:b + 1].contiguous(), parent)
+        assert (O[b].float() - one[0].float()).abs().max() <= 2.0 ** -6 * one.float().abs().max()
+    Q, Kt, Vt, lens = (torch.cat([v, v[:1]]) for v in (Q, Kt, Vt)), 0, 0, np.append(lens, 5).astype(np.int32)
+    Q, Kt, Vt = list(Q)
+    table, indptr = torch.cat([table, table[:2]]), torch.arange(0, 2 * B + 3, 2, dtype=torch.int32, device="cuda")
+    with pytest.raises(S.SpecrollError):
+        call(B + 1)
+
+
+def test_more_than_128_query_heads_a_cache_head_are_refused():
+    x = _case(1, 1, 129, 1, 64, [10], seed=22)
+    with pytest.raises(S.SpecrollError):
+        _run(x, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+
+
+def test_outputs_from_the_ordinary_allocator():
+    """Arrays that share an allocation: sizes, types, alignment, and none on top of another."""
+    from paper_2608_04962_b200 import binding
+    args = _plan_args(np.random.default_rng(7), 37, 900, 400, 0.2, 2)
+    want = ref.page_plan(*args[:5], int(args[5][0]), 333, 4001)
+    binding.set_allocator(None)
+    p = S.page_plan(*[dev(a) for a in args], 333, 4001)
+    for k in ("page_table", "page_indptr", "tok_indptr", "slot_map", "free_list"):
+        assert np.array_equal(host(p[k]), want[k]) and p[k].data_ptr() % 256 == 0 and p[k].is_contiguous(), k
+    spans = sorted((v.data_ptr(), v.data_ptr() + v.numel() * v.element_size()) for v in p.values())
+    assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])) and p["slot_map"].dtype == torch.int64
+    pool = torch.full((2, 3, 2, S.kv4_tile_bytes(64)), 0x99, dtype=torch.uint8, device="cuda")
+    k, v = S.kv4_load(pool, torch.tensor([3, -1, 200], device="cuda"))
+    k.zero_()
+    assert v.shape == (3, 3, 64) and bool((v[0] != 0).all()) and not v[1].any() and bool((v[2] != 0).all())
+    assert v.clone().data_ptr() != v.data_ptr() and (v + 0).shape == v.shape  # (an ordinary tensor to torch)
