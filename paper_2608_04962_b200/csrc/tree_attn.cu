@@ -535,7 +535,9 @@ __global__ void __launch_bounds__(128) attn_combine_kernel(AttnArgs a) {
 // ------------------------------------------------------------------------------ host side
 
 constexpr int PLAN_SMS = 148;  // SMs the chunking is planned for
-constexpr int KV4_FEW_ROWS = 16;  // 4-bit cache: query rows per KV head up to which the mma.sync kernel takes the call
+// 4-bit cache: query rows per KV head up to which the mma.sync kernel takes the call.  148 sequences of 2048 tokens, two KV heads, microseconds
+// with it and with the tcgen05 kernel: 6 rows 38 and 69, 9 rows 54 and 69, 16 rows 56 and 69; 24 rows (two blocks) 83 and 69, 32 rows 77 and 69.
+constexpr int KV4_FEW_ROWS = 16;
 
 // Chunks of the sequences (tile counts) when none may hold more than ct tiles, and the most a sequence has.
 static long long count_chunks(const std::vector<int> &tiles, int ct, int *max_ns) {
@@ -556,10 +558,10 @@ static bool merge_by_kernel(long long units, int max_ns) { return max_ns >= 5 ||
 
 // Estimated finishing time, in quarter tiles (about a third of a microsecond), of the persistent tcgen05 kernel when
 // sequences of the given tile counts (sorted, longest first) are cut into chunks of at most ct tiles: work units go, in
-// the order the device uses, to whichever of `places` CTAs is free first.  A unit costs its K/V tiles, one more for the
+// the order the device uses, to whichever of PLAN_SMS CTAs is free first.  A unit costs its K/V tiles, one more for the
 // tree tile of a sequence's last chunk, one for the hand-over between units; a chunk of a split sequence adds one
 // for its partial, and the last one the merge when the attention kernel does it, else the merge kernel follows.
-static long long estimate_makespan(const std::vector<int> &tiles, int ct, int copies, int places) {
+static long long estimate_makespan(const std::vector<int> &tiles, int ct, int copies) {
     struct Chunk { int tps, cost; };
     std::vector<Chunk> chunks;
     int max_ns = 1;
@@ -577,7 +579,7 @@ static long long estimate_makespan(const std::vector<int> &tiles, int ct, int co
     }
     std::stable_sort(chunks.begin(), chunks.end(), [](const Chunk &x, const Chunk &y) { return x.tps > y.tps; });
     std::priority_queue<long long, std::vector<long long>, std::greater<long long>> sms;
-    for (int i = 0; i < places; ++i) sms.push(0);
+    for (int i = 0; i < PLAN_SMS; ++i) sms.push(0);
     long long end = 0;
     for (const Chunk &c : chunks)
         for (int k = 0; k < copies; ++k) {
@@ -587,6 +589,38 @@ static long long estimate_makespan(const std::vector<int> &tiles, int ct, int co
             end = std::max(end, t);
         }
     return end + ((max_ns > 1 && !merge_inline) ? 8 + max_ns / 2 : 0);
+}
+
+// The same for the 4-bit cache's kernel of few rows, which has a CTA for every unit and `places` of them side by side, without playing
+// through the hand-out (0.5 ms of the host for 256 sequences, where the layer takes 0.05): units that all have a place end with the
+// longest; up to two to a place the shortest of the first are followed by the longest of the others; more even out.
+static long long estimate_few(const std::vector<int> &tiles, int ct, int copies, int places) {
+    std::vector<int> units_of_cost;  // [cost in quarter tiles], units of one copy
+    long long units = 0, sum = 0;
+    int max_ns = 1;
+    for (int t : tiles) {
+        const int ns = std::max(1, (t + ct - 1) / ct), tps = (t + ns - 1) / ns, last = t - (ns - 1) * tps;
+        const int extra = ns > 1 ? 8 : 4, cost = 4 * tps + extra, cost_last = 4 * last + extra + 4;
+        if ((int)units_of_cost.size() <= std::max(cost, cost_last)) units_of_cost.resize((size_t)std::max(cost, cost_last) + 1);
+        units_of_cost[(size_t)cost] += ns - 1;
+        units_of_cost[(size_t)cost_last] += 1;
+        units += ns;
+        sum += (long long)(ns - 1) * cost + cost_last;
+        max_ns = std::max(max_ns, ns);
+    }
+    units *= copies;
+    sum *= copies;
+    // cost of the unit at place i of the order (longest first)
+    std::vector<std::pair<long long, int>> upto;  // (units with this cost or a larger one, cost)
+    long long n = 0;
+    for (int c = (int)units_of_cost.size() - 1; c >= 0; --c)
+        if (units_of_cost[(size_t)c]) upto.emplace_back(n += (long long)units_of_cost[(size_t)c] * copies, c);
+    auto at = [&](long long i) { return std::upper_bound(upto.begin(), upto.end(), std::make_pair(i, 1 << 30))->second; };
+    long long end = at(0);
+    if (units > 2LL * places) end = std::max(end, sum / places + end / 4);
+    else
+        for (long long i = places; i < units; ++i) end = std::max<long long>(end, at(i) + at(2LL * places - 1 - i));
+    return end + (max_ns > 1 ? 8 + max_ns / 2 : 0);
 }
 
 struct AttnPlan {
@@ -671,7 +705,7 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
             for (int i = 0; i < n_seen; ++i)
                 if (seen[i] == c) return;
             seen[n_seen++] = c;
-            const long long m = estimate_makespan(tiles, c, (int)ctas_per_tile, places);
+            const long long m = p->kv4_few ? estimate_few(tiles, c, (int)ctas_per_tile, places) : estimate_makespan(tiles, c, (int)ctas_per_tile);
             if (best < 0 || m < best) {
                 best = m;
                 ct = c;
