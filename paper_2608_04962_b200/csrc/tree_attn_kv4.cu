@@ -14,9 +14,9 @@
 // shared memory at the end.  The tree's bf16 rows are done by the warps before their slices, sixteen nodes each.
 // What bounds it: long sequences take an SM 0.50 us a page and head (17 KB, 0.39 at HBM's rate: 79 %; without decoding 0.42).  Decoding
 // is some 80 integer and 64 packed floating operations a thread for 16 tokens, which the tensor operations and the rest do not quite hide;
-// more warps on an SM (five CTAs at 96 registers) changed
-// nothing, nor did whole pages by one copy each into stages that the four warps share.  A unit takes 12 us beyond its pages: lengths, page table, pages, then the
-// warps' meeting, each a round trip, of which the other three CTAs of the SM hide a part.
+// more warps on an SM (five CTAs at 96 registers) changed nothing, nor did whole pages by one copy each into stages that the four
+// warps share.  A unit takes 12 us beyond its pages: lengths, page table, pages, then the warps' meeting, each a round trip, of which
+// the other three CTAs of the SM hide a part.
 #include <math.h>
 
 #include "kv4.cuh"
