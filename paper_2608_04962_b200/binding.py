@@ -287,7 +287,7 @@ def page_plan(kv_len, add, page_table, page_indptr, free_list, n_free, table_cap
     """specroll_page_plan: page tables, the slots of add[b] new tokens a sequence, and the free list afterwards (all device
     int32, slot_map int64).  ``table_cap``: entries of the new table; ``slot_cap``: new tokens (sum of the positive add).
     Returns page_table [table_cap], page_indptr [B+1], tok_indptr [B+1], slot_map [slot_cap], free_list (as long as the given
-    one), n_free [1]."""
+    one), n_free [1]: views of one allocation, so that any of them that is kept keeps them all."""
     return _n().page_plan(kv_len, add, page_table, page_indptr, free_list, n_free, table_cap, slot_cap, status, out)
 
 
