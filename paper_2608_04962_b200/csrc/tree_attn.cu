@@ -126,9 +126,9 @@ attn_prep_kernel(const int32_t *__restrict__ kv_indptr, const int32_t *__restric
 #ifdef SPECROLL_CHECK
             if (L < 0) {
                 SR_CHECK_FAIL(lane);
-                L = 0;
             }
 #endif
+            L = max(L, 0);  // (a plan of fewer tiles than none would have the roles of the attention kernel wait for one another)
             const int kv0 = lane < B ? (kv_len ? page_indptr[lane] : kv_indptr[lane]) : 0;
             const int tiles = (L + tile_tokens - 1) / tile_tokens;
             const int ns = lane < B ? max(1, (tiles + chunk_tiles - 1) / chunk_tiles) : 0, cost = (tiles + max(ns, 1) - 1) / max(ns, 1);
@@ -179,9 +179,9 @@ attn_prep_kernel(const int32_t *__restrict__ kv_indptr, const int32_t *__restric
 #ifdef SPECROLL_CHECK
         if (L[q] < 0) {  // the device copy of the lengths disagrees with any host copy the planner can have seen
             SR_CHECK_FAIL(b);
-            L[q] = 0;
         }
 #endif
+        L[q] = max(L[q], 0);  // (the keys below have to be at least 0)
     }
 #pragma unroll
     for (int q = 0; q < PASSES; ++q) {

@@ -560,3 +560,13 @@ def test_outputs_from_the_ordinary_allocator():
     k.zero_()
     assert v.shape == (3, 3, 64) and bool((v[0] != 0).all()) and not v[1].any() and bool((v[2] != 0).all())
     assert v.clone().data_ptr() != v.data_ptr() and (v + 0).shape == v.shape  # (an ordinary tensor to torch)
+
+
+@pytest.mark.parametrize("N,Hq", [(1, 4), (24, 12)])
+@pytest.mark.parametrize("B", [3, 40])
+def test_a_negative_length_on_the_device_counts_as_none(B, N, Hq):
+    x = _case(B, N, Hq, 2, 64, [0 if b % 3 == 1 else 130 + b for b in range(B)], seed=21)
+    want = _run(x)
+    t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(np.where(x["len"] > 0, x["len"], -1000).astype(np.int32)),
+         x["len"], dev_bf16(x["Kt"]), dev_bf16(x["Vt"])]
+    assert torch.equal(S.tree_attn_kv4(*t, x["parent"], check_status=True), want)
