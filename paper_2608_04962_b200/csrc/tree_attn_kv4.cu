@@ -537,8 +537,11 @@ __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     const int b = blockIdx.x, hkv = blockIdx.y, part = threadIdx.x / ITEMS, row = threadIdx.x % ROWS, d4 = blockIdx.z * COLS + threadIdx.x % ITEMS / ROWS;
     const int len = max(__ldg(a.kv_len + b), 0);
     const int n_splits = ((len + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS + a.chunk_tiles - 1) / a.chunk_tiles;
-    if (n_splits < 2) return;
+    // (blocks with nothing to do leave their places to those that have, but for one: where no block waited, the kernel after this one would
+    // not wait for the attention kernel)
+    if (n_splits < 2 && (blockIdx.x | blockIdx.y | blockIdx.z) != 0) return;
     pdl_wait();
+    if (n_splits < 2) return;
     const int item0 = __ldcg(a.item_start + b);
     if (item0 < 0 || item0 + n_splits > a.items) return;  // (lengths that are not the host's)
     for (int rb = 0; rb < a.n_rb; ++rb) {

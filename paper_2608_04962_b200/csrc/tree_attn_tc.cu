@@ -1447,8 +1447,10 @@ __global__ void __launch_bounds__(128 * MERGE_PARTS) attn_merge_tc_kernel(AttnAr
     // (19 of 20 blocks otherwise hold the places of the ones that work until the partials are there).
     const int4 e0 = __ldcg(reinterpret_cast<const int4 *>(a.unit_tab) + 2 * (size_t)blockIdx.x);
     const int b = e0.x, n_splits = e0.z, item0 = e0.w;
-    if (e0.y != 0 || n_splits < 2) return;
+    // (one block waits in any case: where none did, the kernel after this one would not wait for the attention kernel)
+    if ((e0.y != 0 || n_splits < 2) && (blockIdx.x | blockIdx.y | blockIdx.z) != 0) return;
     pdl_wait();
+    if (e0.y != 0 || n_splits < 2) return;
     const int hkv = blockIdx.y / a.n_rb, rb = blockIdx.y % a.n_rb;
     const int row = threadIdx.x & 127, part = threadIdx.x >> 7;
     const int gr = rb * a.rows_per_block + row;

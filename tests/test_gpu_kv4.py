@@ -570,3 +570,25 @@ def test_a_negative_length_on_the_device_counts_as_none(B, N, Hq):
     t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(np.where(x["len"] > 0, x["len"], -1000).astype(np.int32)),
          x["len"], dev_bf16(x["Kt"]), dev_bf16(x["Vt"])]
     assert torch.equal(S.tree_attn_kv4(*t, x["parent"], check_status=True), want)
+
+
+@pytest.mark.parametrize("N,Hq,lengths", [(1, 4, [128, 100, 1, 0]), (1, 4, [9000, 0, 6900, 1]), (8, 4, [5000, 129, 0, 9100]), (1, 32, [1, 2, 3, 4])])
+def test_lengths_below_the_hosts(N, Hq, lengths):
+    """A call planned for the longest that the sequences get, as one that was captured, follows the lengths on the device; and what reads its
+    outputs next waits for them, also where nothing is cut any more and the merge has no work."""
+    x = _case(4, N, Hq, 2, 128, [9000, 8000, 7000, 9100], seed=22)
+    y = dict(x, len=np.array(lengths, np.int32), K=[k[:n] for k, n in zip(x["K"], lengths)], V=[v[:n] for v, n in zip(x["V"], lengths)])
+    want, _, A, dot = ref.tree_attn64(_f64(y["Q"]), y["K"], y["V"], y["len"], _f64(y["Kt"]), _f64(y["Vt"]), y["parent"], 128 ** -0.5)
+    tol = 2.0 ** -8 * (A + np.abs(want)) + 2 * (128 * 2.0 ** -23 * dot + 2.0 ** -18) * A + 1e-30   # as in _check
+    t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(y["len"]), x["len"], dev_bf16(x["Kt"]), dev_bf16(x["Vt"])]
+    out = torch.zeros_like(t[0])
+    rows, slots = out.view(4 * N, Hq, 128), torch.arange(4 * N, device="cuda")
+    pools = [torch.zeros((1, Hq, 2, S.kv4_tile_bytes(128)), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    for _ in range(20):
+        out.zero_()
+        S.tree_attn_kv4(*t, x["parent"], out=out)
+        S.kv4_store(rows, rows, slots, pools[0])
+        torch.cuda.synchronize()
+        S.kv4_store(rows, rows, slots, pools[1])
+        assert torch.equal(*pools)
+        assert (np.abs(host(out.double()) - want) <= tol).all()
