@@ -275,8 +275,9 @@ int specroll_gather_hidden(int32_t B, int32_t N, int32_t d, const void *hidden,
  * slot_map[tok_indptr[b] + i] = page * 128 + place is the slot of position kv_len[b] + i, i < add[b], as
  * specroll_kv4_store takes it; free_list_out[free_cap] and *n_free_out.  Entries behind the last one are -1 in all three arrays,
  * and so are pages that the free list did not have and the slots on them.  When it runs out, or an array is too short (what does
- * not fit is not written), *status (device word, nullable; never cleared here) becomes SPECROLL_ELIMIT.
- * n_table: entries of page_table (it is not read beyond them).  Outputs must not overlap inputs.
+ * not fit is not written), *status (device word, nullable; never cleared here) becomes SPECROLL_ELIMIT; the state to go on from is
+ * then the old one (a page -1 in a table is a page like any other here: it would go back to the free list).
+ * n_table: entries of page_table (it is not read beyond them).  Outputs must not overlap inputs or one another.
  * All pointers device; slot_map i64 and 16-byte aligned, the others i32; B <= 4096 (else SPECROLL_ELIMIT), free_cap <= 2^24.
  * With B = 0 the tables are empty and the free list stays as it is. */
 int specroll_page_plan(int32_t B, const int32_t *kv_len, const int32_t *add, const int32_t *page_table, int32_t n_table,

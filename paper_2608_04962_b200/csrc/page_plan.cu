@@ -202,11 +202,18 @@ extern "C" int specroll_page_plan(int32_t B, const int32_t *kv_len, const int32_
         (free_cap && (!free_list || !free_list_out)) || (n_table && !page_table) || (B && (!kv_len || !add || !page_indptr)))
         return SPECROLL_EINVAL;
     if (!aligned16(slot_map)) return SPECROLL_EALIGN;
-    // blocks read the old state while others write the new one
-    const auto meet = [](const int32_t *x, long long nx, const int32_t *y, long long ny) { return x && y && x < y + ny && y < x + nx; };
-    if (meet(page_table, n_table, page_table_out, table_cap) || meet(free_list, free_cap, free_list_out, free_cap) || meet(n_free, 1, n_free_out, 1) ||
-        meet(page_indptr, (long long)B + 1, page_indptr_out, (long long)B + 1))
-        return SPECROLL_EINVAL;
+    // blocks read the old state while others write the new one: no output meets an input or another output
+    struct Span {
+        uintptr_t at, bytes;
+    };
+    const auto span = [](const void *x, long long n, size_t size) { return Span{reinterpret_cast<uintptr_t>(x), x ? (uintptr_t)n * size : 0}; };
+    const Span spans[] = {span(page_table_out, table_cap, 4), span(page_indptr_out, B + 1LL, 4), span(tok_indptr, B + 1LL, 4), span(slot_map, slot_cap, 8),
+                          span(free_list_out, free_cap, 4), span(n_free_out, 1, 4), span(status, 1, 4), span(kv_len, B, 4), span(add, B, 4),
+                          span(page_table, n_table, 4), span(page_indptr, B ? B + 1LL : 0, 4), span(free_list, free_cap, 4), span(n_free, 1, 4)};
+    constexpr int OUTS = 7, SPANS = sizeof(spans) / sizeof(spans[0]);
+    for (int i = 0; i < OUTS; ++i)
+        for (int j = i + 1; j < SPANS; ++j)
+            if (spans[i].bytes && spans[j].bytes && spans[i].at < spans[j].at + spans[j].bytes && spans[j].at < spans[i].at + spans[i].bytes) return SPECROLL_EINVAL;
     const size_t smem = plan_smem(B);
     int n_sm = 0;
     const int rc = device_setup(reinterpret_cast<const void *>(page_plan_kernel), (int)plan_smem(PLAN_MAX_B), &n_sm);

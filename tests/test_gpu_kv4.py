@@ -87,6 +87,19 @@ def test_page_plan_into_the_callers_arrays_and_its_refusals():
         S.page_plan(*args, 100, 4000, out=dict(b, free_list=args[4]))
 
 
+def test_page_plan_refuses_arrays_that_overlap():
+    args = [dev(a) for a in _plan_args(np.random.default_rng(6), 9, 900, 400, 0.2, 2)]
+    out = S.page_plan(*args, 100, 4000)
+    words = out["slot_map"].view(torch.int32)
+    for bad in (dict(tok_indptr=out["page_indptr"]), dict(page_table=words[8:108]), dict(n_free=out["tok_indptr"][3:4]), dict(n_free=args[0][:1]),
+                dict(tok_indptr=args[3]), dict(page_indptr=args[4][:10])):
+        with pytest.raises(S.SpecrollError):
+            S.page_plan(*args, 100, 4000, out=dict(out, **bad))
+    with pytest.raises(S.SpecrollError):
+        S.page_plan(*args, 100, 4000, status=out["n_free"], out=out)
+    S.page_plan(*args, 100, 4000, status=torch.zeros(1, dtype=torch.int32, device="cuda"), out=dict(out, page_table=words[:100], slot_map=torch.empty_like(out["slot_map"])))
+
+
 # ------------------------------------------------------------------ writing and reading
 
 def _blocks(g, T, H, D):
