@@ -646,9 +646,9 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     p->kv4_few = p->use_tc && kv4 && p->rows <= KV4_FEW_ROWS;
     int places = PLAN_SMS;  // CTAs that run side by side
     if (p->kv4_few) {
-        // 8 or 16 rows a CTA
+        // 8 or 16 rows, all in one CTA
         p->rows_per_block = p->rows <= 8 ? 8 : 16;
-        p->n_rb = (p->rows + p->rows_per_block - 1) / p->rows_per_block;
+        p->n_rb = 1;
         p->nodes_per_block = 0;
         places *= p->rows_per_block == 8 ? KV4_CTAS_8 : KV4_CTAS_16;
     } else if (p->use_tc) {

@@ -1,6 +1,6 @@
 // Tree attention over the 4-bit paged cache, for few query rows per KV head: single tokens and small trees.
 //
-// A CTA takes one chunk of a sequence's pages for one KV head and up to 8 R8 query rows (rows = nodes x query heads of the KV head).
+// A CTA takes one chunk of a sequence's pages for one KV head and all its query rows, at most 8 R8 (nodes x query heads of the KV head).
 // Its four warps go through slices of 32 tokens, each for itself: a warp's first thread fetches its slices (K and V codes and scales)
 // with untiled bulk copies into three stages of its own, so that no warp waits for another before the end.  Codes are decoded
 // straight into mma.sync fragments: a cached element passes through shared memory once, as four bits, and is decoded once for all rows:
@@ -73,10 +73,10 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     pdl_wait();
     pdl_launch_dependents();
 
-    // ---- the unit: (chunk, KV head, row block).  Chunks are counted in the order of the sequences; every CTA finds its own from the
+    // ---- the unit: (chunk, KV head).  Chunks are counted in the order of the sequences; every CTA finds its own from the
     // lengths (a plan made by a kernel in front took ten microseconds for 256 sequences).
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;  // (seconds ahead of any wait that could run out)
-    const int rb = (int)blockIdx.x % a.n_rb, hkv = (int)blockIdx.x / a.n_rb % a.Hkv, item = (int)blockIdx.x / a.n_rb / a.Hkv;
+    const int hkv = (int)blockIdx.x % a.Hkv, item = (int)blockIdx.x / a.Hkv;
     int b = item, split = 0, n_splits = 1, L, slot0;
     if (a.items == a.B) {  // (nothing is cut)
         L = max(__ldg(a.kv_len + b), 0);
@@ -119,7 +119,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     found[2] = ns;
                     found[3] = len;
                     found[4] = i - b0 == 0 ? pages[0] : i - b0 == 1 ? pages[1] : i - b0 == 2 ? pages[2] : i - b0 == 3 ? pages[3] : __ldg(a.page_indptr + i);
-                    if (item == at && hkv == 0 && rb == 0) a.item_start[i] = at;  // (for the merge)
+                    if (item == at && hkv == 0) a.item_start[i] = at;  // (for the merge)
                     break;
                 }
                 at += ns;
@@ -138,7 +138,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     const int tps = (tiles_b + n_splits - 1) / n_splits;
     const int t_lo = min(tiles_b, split * tps), n_t = min(tiles_b, t_lo + tps) - t_lo;
     const bool has_tree = split == n_splits - 1;
-    const int N = a.N, G = a.G, row0 = rb * C::ROWS;
+    const int N = a.N, G = a.G;
     // this warp's slices: slice i is the 32 tokens of the sequence from first + STRIDE i on, a quarter of a page
     constexpr int STRIDE = WARPS * SLICE;
     const int first = t_lo * SPECROLL_PAGE_TOKENS + warp * SLICE, end = min(L, (t_lo + n_t) * SPECROLL_PAGE_TOKENS);
@@ -191,7 +191,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         uint32_t qf[R8][2 * C::STEPS];
 #pragma unroll
         for (int r = 0; r < R8; ++r) {
-            const int gr = row0 + 8 * r + g;
+            const int gr = 8 * r + g;
             const bool ok = gr < a.rows;
             const int n = ok ? gr / G : 0, gq = ok ? gr % G : 0;
             const uint4 *src = reinterpret_cast<const uint4 *>(a.Q + (((size_t)b * N + n) * a.Hq + hkv * G + gq) * D + C::RUN * c);
@@ -332,7 +332,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             uint32_t pf[1][R8][2];
             const int n0 = 16 * warp + k_tok;
             softmax(s, a.scale_log2, 1.0f / KV4_UP, true, false, [&](int, int r, int e) {
-                const int gr = row0 + 8 * r + 2 * c + (e & 1);
+                const int gr = 8 * r + 2 * c + (e & 1);
                 return gr < a.rows && ((mask.anc[gr / G] >> (n0 + (e & 2 ? 8 : 0))) & 1ull);
             }, pf);
 #pragma unroll
@@ -480,8 +480,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     }
     __syncthreads();
     for (int i = threadIdx.x; i < C::ROWS * (D / 4); i += THREADS) {
-        const int row = i % C::ROWS, d4 = i / C::ROWS, gr = row0 + row;
-        if (gr >= a.rows) continue;
+        const int row = i % C::ROWS, d4 = i / C::ROWS;
+        if (row >= a.rows) continue;
         float M = -INFINITY;
 #pragma unroll
         for (int q = 0; q < WARPS; ++q) M = fmaxf(M, jm[q * C::ROWS + row]);
@@ -498,7 +498,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             acc.w += f * x.w;
         }
         acc = make_float4(acc.x * KV4_UP, acc.y * KV4_UP, acc.z * KV4_UP, acc.w * KV4_UP);
-        const int n = gr / G, gq = gr % G;
+        const int n = row / G, gq = row % G;
         if (n_splits == 1) {
             const float inv = sum > 0.f ? 1.0f / sum : 0.f;
             const size_t at = ((size_t)b * N + n) * a.Hq + hkv * G + gq;
@@ -507,8 +507,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             if (a.lse && d4 == 0) a.lse[at] = (M + log2f(sum)) * 0.6931471805599453f;
         } else {
             const size_t unit = (size_t)item * a.Hkv + hkv;
-            reinterpret_cast<float4 *>(a.part_o)[(unit * (D / 4) + d4) * a.rows_pad + gr] = acc;
-            if (d4 == 0) reinterpret_cast<float2 *>(a.part_ml)[unit * a.rows_pad + gr] = make_float2(M, sum);
+            reinterpret_cast<float4 *>(a.part_o)[(unit * (D / 4) + d4) * a.rows_pad + row] = acc;
+            if (d4 == 0) reinterpret_cast<float2 *>(a.part_ml)[unit * a.rows_pad + row] = make_float2(M, sum);
         }
     }
 }
@@ -544,66 +544,62 @@ __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     if (n_splits < 2) return;
     const int item0 = __ldcg(a.item_start + b);
     if (item0 < 0 || item0 + n_splits > a.items) return;  // (lengths that are not the host's)
-    for (int rb = 0; rb < a.n_rb; ++rb) {
-        const int gr = rb * ROWS + row;
-        const size_t unit = (size_t)item0 * a.Hkv + hkv;
-        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + unit * a.rows_pad + gr;
-        const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + (unit * (D / 4) + d4) * a.rows_pad + gr;
-        const size_t step_ml = (size_t)a.Hkv * a.rows_pad, step_o = step_ml * (D / 4);
-        float M = -INFINITY, sum = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const size_t unit = (size_t)item0 * a.Hkv + hkv;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + unit * a.rows_pad + row;
+    const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + (unit * (D / 4) + d4) * a.rows_pad + row;
+    const size_t step_ml = (size_t)a.Hkv * a.rows_pad, step_o = step_ml * (D / 4);
+    float M = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-        for (int i0 = part; i0 < n_splits; i0 += STEP * PARTS) {
-            float2 v[STEP];
-            float4 x[STEP];
+    for (int i0 = part; i0 < n_splits; i0 += STEP * PARTS) {
+        float2 v[STEP];
+        float4 x[STEP];
 #pragma unroll
-            for (int i = 0; i < STEP; ++i) {
-                const size_t s = (size_t)min(i0 + i * PARTS, n_splits - 1);  // (a chunk beyond the last: weight zero below)
-                v[i] = __ldcg(ml + s * step_ml);
-                x[i] = __ldcg(po + s * step_o);
-            }
-            float top = M;
-#pragma unroll
-            for (int i = 0; i < STEP; ++i) top = fmaxf(top, v[i].x);
-            const float f = M == -INFINITY ? 0.f : ex2_approx(M - top);
-            M = top;
-            sum *= f;
-            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-#pragma unroll
-            for (int i = 0; i < STEP; ++i) {
-                const float w = (i0 + i * PARTS >= n_splits || v[i].x == -INFINITY) ? 0.f : ex2_approx(v[i].x - M);
-                sum += w * v[i].y;
-                acc.x += w * x[i].x;
-                acc.y += w * x[i].y;
-                acc.z += w * x[i].z;
-                acc.w += w * x[i].w;
-            }
+        for (int i = 0; i < STEP; ++i) {
+            const size_t s = (size_t)min(i0 + i * PARTS, n_splits - 1);  // (a chunk beyond the last: weight zero below)
+            v[i] = __ldcg(ml + s * step_ml);
+            x[i] = __ldcg(po + s * step_o);
         }
-        sh_ml[threadIdx.x] = make_float2(M, sum);
-        sh_acc[threadIdx.x] = acc;
-        __syncthreads();
-        if (part == 0 && gr < a.rows) {
+        float top = M;
 #pragma unroll
-            for (int q = 1; q < PARTS; ++q) M = fmaxf(M, sh_ml[q * ITEMS + threadIdx.x].x);
-            sum = 0.f;
-            acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < STEP; ++i) top = fmaxf(top, v[i].x);
+        const float f = M == -INFINITY ? 0.f : ex2_approx(M - top);
+        M = top;
+        sum *= f;
+        acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) {
-                const float2 e = sh_ml[q * ITEMS + threadIdx.x];
-                const float4 y = sh_acc[q * ITEMS + threadIdx.x];
-                const float w = e.x == -INFINITY ? 0.f : ex2_approx(e.x - M);
-                sum += w * e.y;
-                acc.x += w * y.x;
-                acc.y += w * y.y;
-                acc.z += w * y.z;
-                acc.w += w * y.w;
-            }
-            const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-            const size_t at = ((size_t)b * a.N + gr / a.G) * a.Hq + hkv * a.G + gr % a.G;
-            *reinterpret_cast<uint2 *>(a.O + at * D + 4 * d4) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-            if (a.lse && d4 == 0) a.lse[at] = (M + log2f(sum)) * 0.6931471805599453f;
+        for (int i = 0; i < STEP; ++i) {
+            const float w = (i0 + i * PARTS >= n_splits || v[i].x == -INFINITY) ? 0.f : ex2_approx(v[i].x - M);
+            sum += w * v[i].y;
+            acc.x += w * x[i].x;
+            acc.y += w * x[i].y;
+            acc.z += w * x[i].z;
+            acc.w += w * x[i].w;
         }
-        __syncthreads();
+    }
+    sh_ml[threadIdx.x] = make_float2(M, sum);
+    sh_acc[threadIdx.x] = acc;
+    __syncthreads();
+    if (part == 0 && row < a.rows) {
+#pragma unroll
+        for (int q = 1; q < PARTS; ++q) M = fmaxf(M, sh_ml[q * ITEMS + threadIdx.x].x);
+        sum = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            const float2 e = sh_ml[q * ITEMS + threadIdx.x];
+            const float4 y = sh_acc[q * ITEMS + threadIdx.x];
+            const float w = e.x == -INFINITY ? 0.f : ex2_approx(e.x - M);
+            sum += w * e.y;
+            acc.x += w * y.x;
+            acc.y += w * y.y;
+            acc.z += w * y.z;
+            acc.w += w * y.w;
+        }
+        const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+        const size_t at = ((size_t)b * a.N + row / a.G) * a.Hq + hkv * a.G + row % a.G;
+        *reinterpret_cast<uint2 *>(a.O + at * D + 4 * d4) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (a.lse && d4 == 0) a.lse[at] = (M + log2f(sum)) * 0.6931471805599453f;
     }
 }
 
