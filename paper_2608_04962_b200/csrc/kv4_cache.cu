@@ -74,13 +74,6 @@ __device__ __forceinline__ uint32_t kv4_encode(const uint4 &x, uint32_t &scale) 
     return __byte_perm(even, odd, 0x5410);
 }
 
-// Codes and scale of eight elements to their places: word `at` of row `row` of a tile.
-template <int D>
-__device__ __forceinline__ void kv4_put(uint8_t *tile, int row, int at, uint32_t codes, uint32_t scale) {
-    *reinterpret_cast<uint32_t *>(tile + row * Kv4<D>::ROW + at * 4) = codes;
-    if ((at & 3) == 0) tile[Kv4<D>::CODES + row * Kv4<D>::SROW + (at >> 2)] = (uint8_t)scale;
-}
-
 constexpr int KV4_THREADS = 256, KV4_EACH = 4;  // words of 16 bytes of bf16 that a thread takes side by side
 
 // What the two kernels by slot share out.  A thread has one word of K or of V of its tokens for good (a token has `columns` = 2 Hkv D / 8
@@ -189,8 +182,7 @@ struct Kv4Layers {
 
 // grid = (B, groups of `each` layers): the committed rows of sequence b go to cache positions kv_len[b] + i of those layers' pools, as
 // commit_path_kernel has it for a bf16 cache.  The first warp finds the rows' places, once for K, V and all layers of the group (a block
-// for every row and layer spent its time on that chain of loads: 40 us instead of 13 for 256 sequences, 28 layers of two heads);
-// a thread then takes four words at a time.
+// for every row and layer spent its time on that chain of loads); a thread then has one column, as above, and takes four words at a time.
 template <int D>
 __global__ void __launch_bounds__(KV4_THREADS)
 kv4_commit_kernel(const __grid_constant__ Kv4Layers lay, const int32_t *__restrict__ path_node, const int32_t *__restrict__ n_acc,
@@ -198,7 +190,8 @@ kv4_commit_kernel(const __grid_constant__ Kv4Layers lay, const int32_t *__restri
                   const int32_t *__restrict__ kv_len, int N, int K, int Hkv, int n_layers, int each, int32_t *__restrict__ status,
                   int32_t *__restrict__ kv_len_out) {
     constexpr int W = D / 8;
-    __shared__ long long sh_src[SPECROLL_MAX_HEADS + 1], sh_dst[SPECROLL_MAX_HEADS + 1];  // first word of the tree row; slot
+    __shared__ long long sh_src[SPECROLL_MAX_HEADS + 1], sh_page[SPECROLL_MAX_HEADS + 1];  // first word of the tree row; first byte of the page
+    __shared__ uint32_t sh_row[SPECROLL_MAX_HEADS + 1];
     __shared__ int sh_rows;
     pdl_wait();
     pdl_launch_dependents();
@@ -218,7 +211,8 @@ kv4_commit_kernel(const __grid_constant__ Kv4Layers lay, const int32_t *__restri
         if (ok) {
             const int r = __popc(have & ((1u << i) - 1u));
             sh_src[r] = ((long long)b * N + node) * Hkv * W;
-            sh_dst[r] = (long long)page * SPECROLL_PAGE_TOKENS + pos % SPECROLL_PAGE_TOKENS;
+            sh_page[r] = (long long)page * Hkv * (2 * Kv4<D>::TILE);
+            sh_row[r] = (uint32_t)(pos % SPECROLL_PAGE_TOKENS);
         }
         if (i == 0) {
             sh_rows = __popc(have);
@@ -226,30 +220,35 @@ kv4_commit_kernel(const __grid_constant__ Kv4Layers lay, const int32_t *__restri
         }
     }
     __syncthreads();
-    // words in the order (layer, row, K or V, head, word of the head)
-    const int heads = Hkv * W, l0 = blockIdx.y * each, per_layer = sh_rows * 2 * heads, total = per_layer * min(each, n_layers - l0);
-    for (int i0 = threadIdx.x; i0 - (int)threadIdx.x < total; i0 += KV4_THREADS * KV4_EACH) {
-        uint4 x[KV4_EACH];
-        uint8_t *tile[KV4_EACH];
-        int row[KV4_EACH], at[KV4_EACH];
+    // a thread has one word of K or V (or several, KV4_THREADS apart) of `side` (layer, row) pairs side by side and goes through the pairs
+    const uint32_t words = (uint32_t)(Hkv * W), columns = 2 * words, rows = (uint32_t)sh_rows, l0 = blockIdx.y * each;
+    const uint32_t pairs = rows * (uint32_t)min(each, n_layers - (int)l0), side = max(1u, KV4_THREADS / columns);
+    const uint32_t first = columns < KV4_THREADS ? threadIdx.x / columns : 0u;
+    const uint32_t per_row = rows ? 65536u / rows + 1u : 0u;  // (pair * per_row >> 16 is pair / rows: pairs are below 2^8)
+    for (uint32_t c0 = 0; c0 < columns; c0 += KV4_THREADS) {
+        const uint32_t col = threadIdx.x - first * columns + c0, v = col >= words, word = v ? col - words : col;
+        const bool on = first < side && col < columns;
+        const uint32_t tile = (word / W * 2 + v) * Kv4<D>::TILE, at = tile + word % W * 4, sat = tile + Kv4<D>::CODES + word % W / 4;
+        for (uint32_t p0 = 0; p0 < pairs; p0 += side * KV4_EACH) {
+            uint4 x[KV4_EACH];
+            uint32_t lr[KV4_EACH];  // layer and row of the pair
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) {
-            const int i = i0 + q * KV4_THREADS;
-            tile[q] = nullptr;
-            x[q] = make_uint4(0u, 0u, 0u, 0u);
-            if (i >= total) continue;
-            const int l = i / per_layer, j = i - l * per_layer, r = j / (2 * heads), w = j - r * 2 * heads, v = w >= heads, word = v ? w - heads : w;
-            const long long slot = sh_dst[r];
-            x[q] = ld_nc_v4((v ? lay.Vt[l0 + l] : lay.Kt[l0 + l]) + sh_src[r] + word);
-            tile[q] = lay.pool[l0 + l] + ((slot / SPECROLL_PAGE_TOKENS * Hkv + word / W) * 2 + v) * (long long)Kv4<D>::TILE;
-            row[q] = (int)(slot % SPECROLL_PAGE_TOKENS);
-            at[q] = word % W;
-        }
+            for (uint32_t q = 0; q < KV4_EACH; ++q) {
+                const uint32_t p = p0 + first + q * side, l = p * per_row >> 16, r = p - l * rows;
+                const bool has = on && p < pairs;
+                lr[q] = has ? l << 8 | r : ~0u;
+                x[q] = has ? ld_nc_v4((v ? lay.Vt[l0 + l] : lay.Kt[l0 + l]) + sh_src[r] + word) : make_uint4(0u, 0u, 0u, 0u);
+            }
 #pragma unroll
-        for (int q = 0; q < KV4_EACH; ++q) {
-            uint32_t scale;
-            const uint32_t codes = kv4_encode(x[q], scale);
-            if (tile[q]) kv4_put<D>(tile[q], row[q], at[q], codes, scale);
+            for (uint32_t q = 0; q < KV4_EACH; ++q) {
+                uint32_t scale;
+                const uint32_t codes = kv4_encode(x[q], scale);  // (four threads a block of 32, all in it together)
+                if (lr[q] == ~0u) continue;
+                uint8_t *const page = lay.pool[l0 + (lr[q] >> 8)] + sh_page[lr[q] & 255u];
+                const uint32_t row = sh_row[lr[q] & 255u];
+                *reinterpret_cast<uint32_t *>(page + (at + row * Kv4<D>::ROW)) = codes;
+                if ((word & 3) == 0) page[sat + row * Kv4<D>::SROW] = (uint8_t)scale;
+            }
         }
     }
 }
