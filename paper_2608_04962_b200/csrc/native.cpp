@@ -248,6 +248,13 @@ class Out {
     PyObject *given_, *dict_;
 };
 
+// The launch goes to the current device's stream: tensors of another one are refused (by the calls that came with the 4-bit cache).
+void here(const char *what, std::initializer_list<const at::Tensor *> ts) {
+    const int device = c10::cuda::current_device();
+    for (const at::Tensor *t : ts)
+        if (t && t->defined() && t->get_device() != device) fail("%s: every tensor must be on the current device (cuda:%d)", what, device);
+}
+
 void *stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
 // The C call itself runs without the interpreter lock, as a ctypes call does.  Its arguments are evaluated before the lock is
@@ -395,6 +402,7 @@ PyObject *tree_attn_kv4(PyObject *const *a) {
     const auto *pt = (const int32_t *)dev(a[2], I32, "page_table"), *pip = (const int32_t *)dev(pi, I32, "page_indptr"), *pkl = (const int32_t *)dev(kl, I32, "kv_len_dev");
     void *po = dev(O, BF16, "out");
     auto *pl = lse.defined() ? (float *)dev(lse, F32, "lse") : nullptr;
+    here("tree_attn_kv4", {&Q, &pool, tensor(a[2], "page_table"), &pi, &kl, &Kt, &Vt, &O, &lse, &ws});
     CALL(specroll_tree_attn_kv4, &desc, pq, pp, (int64_t)pool.size(0), pt, pip, pkl, len.data(), pkt, pvt, parent.data(), po, pl, ptr(ws), bytes_of(ws));
     return attn_result(O, lse, ws);
 }
@@ -414,12 +422,15 @@ PyObject *page_plan(PyObject *const *a) {
     const auto *pl = (const int32_t *)dev(kl, I32, "kv_len"), *pa = (const int32_t *)dev(add, I32, "add"), *ppt = (const int32_t *)dev(pt, I32, "page_table");
     const auto *ppi = (const int32_t *)dev(pi, I32, "page_indptr"), *pf = (const int32_t *)dev(fl, I32, "free_list"), *pn = (const int32_t *)dev(nf, I32, "n_free");
     auto *ps = (int32_t *)dev(st, I32, "status");
+    here("page_plan", {&kl, &add, &pt, &pi, &fl, &nf, st});
     if (a[9] != Py_None) {
         const struct { const char *name; int64_t n; } want[] = {{"page_table", table_cap}, {"page_indptr", B + 1}, {"tok_indptr", B + 1},
                                                                 {"slot_map", slot_cap}, {"free_list", fl.numel()}, {"n_free", 1}};
         for (const auto &w : want) {
             const Ref o(PyMapping_GetItemString(a[9], w.name));
-            if (need(o.o, w.name).numel() != w.n) fail("page_plan: out[%s] must have %lld entries", w.name, (long long)w.n);
+            const at::Tensor &t = need(o.o, w.name);
+            if (t.numel() != w.n) fail("page_plan: out[%s] must have %lld entries", w.name, (long long)w.n);
+            if (t.is_cuda()) here("page_plan", {&t});
         }
     }
     Out out(a[9]);
@@ -460,6 +471,7 @@ PyObject *kv4_store(PyObject *const *a) {
     const auto *ps = (const int64_t *)dev(slots, I64, "slot_map");
     void *pp = dev(pool, U8, "pool");
     auto *pw = (int32_t *)dev(st, I32, "status");
+    here("kv4_store", {&K, &V, &slots, &pool, st});
     CALL(specroll_kv4_store, T, (int32_t)Hkv, (int32_t)D, pk, pv, ps, pp, (int64_t)pool.size(0), pw);
     return Py_NewRef(Py_None);
 }
@@ -486,6 +498,7 @@ PyObject *kv4_load(PyObject *const *a) {
     const auto *ps = (const int64_t *)dev(slots, I64, "slot_map");
     void *pk = dev(kv[0], BF16, "out"), *pv = dev(kv[1], BF16, "out");
     auto *pw = (int32_t *)dev(st, I32, "status");
+    here("kv4_load", {&pool, &slots, &kv[0], &kv[1], st});
     CALL(specroll_kv4_load, T, (int32_t)Hkv, (int32_t)D, pp, (int64_t)pool.size(0), ps, pk, pv, pw);
     return Py_BuildValue("NN", THPVariable_Wrap(kv[0]), THPVariable_Wrap(kv[1]));
 }
@@ -502,6 +515,7 @@ PyObject *commit_path_kv4_layers(PyObject *const *a) {
         seqs.emplace_back(PySequence_Fast(src[i], "commit_path_kv4_layers: one tensor per layer in each list"));
         const Py_ssize_t len = PySequence_Fast_GET_SIZE(seqs.back().o);
         if (i == 0) n = len;
+        ptrs[i].reserve((size_t)len);
         if (len != n || n == 0) fail("commit_path_kv4_layers: one tensor per layer in each list");
         for (Py_ssize_t l = 0; l < n; ++l) {
             const at::Tensor &t = need(PySequence_Fast_GET_ITEM(seqs.back().o, l), names[i], 4);
@@ -509,6 +523,7 @@ PyObject *commit_path_kv4_layers(PyObject *const *a) {
             if (i < 2 ? t.sizes() != first[0]->sizes() : t.sizes() != first[2]->sizes())
                 fail("commit_path_kv4_layers: %s differs in shape between layers", names[i]);
             ptrs[i].push_back(dev(t, i < 2 ? BF16 : U8, names[i]));
+            if (t.get_device() != first[0]->get_device()) fail("commit_path_kv4_layers: %s of layer %zd is on another device", names[i], l);
         }
     }
     const at::Tensor &Kt = *first[0], &pool = *first[2], &path = need(a[2], "path_node", 2);
@@ -520,6 +535,7 @@ PyObject *commit_path_kv4_layers(PyObject *const *a) {
     const auto *pp = (const int32_t *)dev(path, I32, "path_node"), *pn = (const int32_t *)dev(na, I32, "n_acc");
     const auto *pt = (const int32_t *)dev(a[5], I32, "page_table"), *ppi = (const int32_t *)dev(pi, I32, "page_indptr"), *pl = (const int32_t *)dev(kl, I32, "kv_len");
     auto *po = (int32_t *)dev(ko, I32, "kv_len_out"), *ps = (int32_t *)dev(st, I32, "status");
+    here("commit_path_kv4_layers", {&Kt, &path, &na, tensor(a[5], "page_table"), &pi, &kl, ko, st});
     CALL(specroll_commit_path_kv4_layers, (int32_t)B, (int32_t)N, (int32_t)K, (int32_t)Hkv, (int32_t)D, (int32_t)n, ptrs[0].data(), ptrs[1].data(), pp, pn,
          ptrs[2].data(), (int64_t)pool.size(0), pt, ppi, pl, po, ps);
     return Py_NewRef(Py_None);
