@@ -538,6 +538,7 @@ constexpr int PLAN_SMS = 148;  // SMs the chunking is planned for
 // 4-bit cache: query rows per KV head up to which the mma.sync kernel takes the call.  148 sequences of 2048 tokens, two KV heads, microseconds
 // with it and with the tcgen05 kernel: 6 rows 38 and 69, 9 rows 54 and 69, 16 rows 56 and 69; 24 rows (two blocks) 83 and 69, 32 rows 77 and 69.
 constexpr int KV4_FEW_ROWS = 16;
+static_assert(KV4_FEW_ROWS <= 16, "the kernel of few rows has two groups of eight, and one warp for sixteen nodes");
 
 // Chunks of the sequences (tile counts) when none may hold more than ct tiles, and the most a sequence has.
 static long long count_chunks(const std::vector<int> &tiles, int ct, int *max_ns) {

@@ -11,7 +11,7 @@
 // paired by byte permutes before decoding.  Tokens of a pair change places in every other pair, which halves the bank conflicts
 // of V's reads.
 // Every warp has a softmax of its own (reference maximum per row, which stays until a score is 2^8 above it); the four meet in
-// shared memory at the end.  The tree's bf16 rows are done by the warps before their slices, sixteen nodes each.
+// shared memory at the end.  The tree's bf16 rows (sixteen nodes at most) are done by the first warp before its slices.
 // What bounds it: long sequences take an SM 0.50 us a page and head (17 KB, 0.39 at HBM's rate: 79 %; without decoding 0.42).  Decoding
 // is some 80 integer and 64 packed floating operations a thread for 16 tokens, which the tensor operations and the rest do not quite hide;
 // more warps on an SM (five CTAs at 96 registers) changed nothing, nor did whole pages by one copy each into stages that the four
@@ -204,8 +204,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 qf[r][4 * i + 3] = x.w;
             }
         }
-        // the tree's rows of this warp, bf16, sixteen nodes: K rows and V rows as the codes of the cache are divided among the threads
-        const bool tree = has_tree && 16 * warp < N;
+        // the tree's rows, bf16: K rows and V rows as the codes of the cache are divided among the threads
+        const bool tree = has_tree && warp == 0;  // (rows of one KV head: sixteen nodes at most)
         uint4 kx[2][C::RUN / 8], vx[4][C::VRUN / 8];
         // the tokens (of 16) that a thread's indexes stand for: index 2 j + e is token 2 j + (e ^ (j & 1))
         const int k_tok = g ^ ((g >> 1) & 1);               // K rows g and g + 8: tokens k_tok and k_tok + 8
@@ -216,14 +216,14 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int n = 16 * warp + k_tok + 8 * h;
+                const int n = k_tok + 8 * h;
                 const uint4 *src = reinterpret_cast<const uint4 *>(a.Kt + ((rows_of_b + n) * a.Hkv + hkv) * D + C::RUN * c);
 #pragma unroll
                 for (int i = 0; i < C::RUN / 8; ++i) kx[h][i] = n < N ? __ldg(src + i) : zero;
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int n = 16 * warp + ((q & 1) ? v_b : v_a) + 8 * (q >> 1);
+                const int n = ((q & 1) ? v_b : v_a) + 8 * (q >> 1);
                 const uint4 *src = reinterpret_cast<const uint4 *>(a.Vt + ((rows_of_b + n) * a.Hkv + hkv) * D + C::VRUN * g);
 #pragma unroll
                 for (int i = 0; i < C::VRUN / 8; ++i) vx[q][i] = n < N ? __ldg(src + i) : zero;
@@ -330,10 +330,9 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 }
             }
             uint32_t pf[1][R8][2];
-            const int n0 = 16 * warp + k_tok;
             softmax(s, a.scale_log2, 1.0f / KV4_UP, true, false, [&](int, int r, int e) {
                 const int gr = 8 * r + 2 * c + (e & 1);
-                return gr < a.rows && ((mask.anc[gr / G] >> (n0 + (e & 2 ? 8 : 0))) & 1ull);
+                return gr < a.rows && ((mask.anc[gr / G] >> (k_tok + (e & 2 ? 8 : 0))) & 1ull);
             }, pf);
 #pragma unroll
             for (int i = 0; i < C::VRUN / 8; ++i) {
@@ -525,7 +524,8 @@ static int launch_kv4(const AttnArgs &a, const TopoMask &mask, int32_t *status, 
 
 // Sums the chunks of every split sequence.  grid = (B, Hkv, Z): a block has a Z-th of D of all rows of one (sequence, KV head), four floats
 // a thread, and as many parts of the chunks as 256 threads have room for; a part's chunks are taken eight at a time with all their loads
-// in flight.  Z = 4 where some sequence has more chunks than that, else the fewest blocks.  Launched as a programmatic dependent of the
+// in flight.  Z = 4 where some sequence has more than 8 chunks, else the
+// fewest blocks (attention and merge: 8 sequences of 20000 tokens, 32 chunks: 31.3 us with Z = 4, 35.2 with 1; 256 of 1500, at most 8: 52.2 and 47.8).  Launched as a programmatic dependent of the
 // attention kernel, which lets it start only behind its own wait: the lengths can be read ahead of the wait for the partials.
 template <int D, int ROWS, int Z>
 __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
