@@ -284,7 +284,8 @@ static int by_slot(int64_t T, int32_t Hkv, int32_t D, const void *K, const void 
     a->columns = (uint32_t)(2 * Hkv * (D / 8));
     a->page_bytes = (uint32_t)(Hkv * 2 * specroll_kv4_tile_bytes(D));
     a->side = std::max(1u, KV4_THREADS / a->columns);
-    // one word a thread while that is less than a wave of blocks: few tokens are a chain of latencies
+    // one word a thread while that is less than a wave of blocks: few tokens are a chain of latencies (store and load, us: 37 tokens 3.4, with
+    // four words 3.9; 98304 tokens 500 and 197; eight or sixteen, four at a time: 197)
     a->each = T * a->columns > 148LL * 8 * KV4_THREADS ? KV4_EACH : 1;
     grid->x = (unsigned)((T + a->side * a->each - 1) / (a->side * a->each));
     grid->y = (a->columns + KV4_THREADS - 1) / KV4_THREADS;

@@ -524,9 +524,9 @@ static int launch_kv4(const AttnArgs &a, const TopoMask &mask, int32_t *status, 
 
 // Sums the chunks of every split sequence.  grid = (B, Hkv, Z): a block has a Z-th of D of all rows of one (sequence, KV head), four floats
 // a thread, and as many parts of the chunks as 256 threads have room for; a part's chunks are taken eight at a time with all their loads
-// in flight.  Z = 4 where some sequence has more than 8 chunks, else the
-// fewest blocks (attention and merge: 8 sequences of 20000 tokens, 32 chunks: 31.3 us with Z = 4, 35.2 with 1; 256 of 1500, at most 8: 52.2 and 47.8).  Launched as a programmatic dependent of the
-// attention kernel, which lets it start only behind its own wait: the lengths can be read ahead of the wait for the partials.
+// in flight.  Z = 4 where some sequence has more than 8 chunks, else the fewest blocks (attention and merge, us: 8 sequences of 20000
+// tokens, 32 chunks, 31.3 with Z = 4 and 35.2 with 1; 256 of 1500, 8 chunks at most, 52.2 and 47.8).  Launched as a programmatic dependent
+// of the attention kernel, which lets it start only behind its own wait: the lengths can be read ahead of the wait for the partials.
 template <int D, int ROWS, int Z>
 __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     constexpr int COLS = D / 4 / Z, ITEMS = ROWS * COLS, PARTS = 256 / ITEMS, STEP = 8;
