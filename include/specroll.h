@@ -157,7 +157,7 @@ int specroll_tree_draw(int32_t B, int32_t N, int32_t K, int32_t k, float tempera
  * sizes the launch so no device read-back is needed); kv_indptr[0] must be 0 (Kc and Vc point at
  * the first sequence's first token), else SPECROLL_EINVAL; Kt,Vt[B,N,Hkv,D] bf16.
  * Outputs: O[B,N,Hq,D] bf16; lse[B,N,Hq] fp32 or NULL (natural-log sum-exp of the scaled scores).
- * Limits: D == 64 or 128, Hq % Hkv == 0, N <= 64.
+ * Limits: D == 64 or 128, Hq % Hkv == 0, N <= 64, a sequence of at most 2^31 - 128 cached tokens.
  */
 typedef struct {
     int32_t B, N, Hq, Hkv, D;

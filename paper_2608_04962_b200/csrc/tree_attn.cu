@@ -674,7 +674,8 @@ static int compute_attn_plan(const specroll_attn_desc *d, const int32_t *indptr_
     int max_tiles = 0;
     for (int b = 0; b < d->B; ++b) {
         const int L = indptr_host[b + 1] - indptr_host[b];
-        if (L < 0) return SPECROLL_EINVAL;
+        // (tokens are rounded up to whole tiles in 32 bits, here and in the kernels)
+        if (L < 0 || L > INT32_MAX - (TT - 1)) return SPECROLL_EINVAL;
         const int t = (L + TT - 1) / TT;
         tiles_total += t;
         if (t > max_tiles) max_tiles = t;

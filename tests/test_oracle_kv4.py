@@ -131,3 +131,20 @@ def test_the_attention_refuses_on_the_host():
     assert call(B=0) == 0
     assert S.tree_attn_kv4_workspace_bytes(2, 4, 4, 2, 64, lens) > 0
     assert S.tree_attn_kv4_workspace_bytes(2, 4, 4, 2, 96, lens) == 0
+
+
+@pytest.mark.parametrize("N,Hq,Hkv", [(1, 1, 1), (1, 12, 2), (8, 2, 1), (48, 10, 2)])
+def test_lengths_that_round_up_past_31_bits_are_refused(N, Hq, Hkv):
+    """The plan rounds lengths up to whole pages: the longest that still has a rounding is planned, one more is refused on the host."""
+    most = 2 ** 31 - 128
+    for f in (S.tree_attn_kv4_workspace_bytes, S.tree_attn_paged_workspace_bytes):
+        for lens in ([most], [100, most]):
+            assert f(len(lens), N, Hq, Hkv, 128, np.array(lens, np.int32)) > 0
+        for lens in ([most + 1], [2 ** 31 - 1], [0, 2 ** 31 - 50]):
+            assert f(len(lens), N, Hq, Hkv, 128, np.array(lens, np.int32)) == 0
+    parent, lens = np.arange(-1, N - 1, dtype=np.int32), np.array([2 ** 31 - 1], np.int32)
+    ok = C.c_void_p(np.zeros(64, np.int64).ctypes.data // 16 * 16 + 16)
+    d = S.AttnDesc(1, N, Hq, Hkv, 128, 0.1, 0)
+    L = S.lib()
+    assert L.specroll_tree_attn_kv4(C.byref(d), ok, ok, C.c_int64(4), ok, ok, ok, lens.ctypes.data_as(C.c_void_p), ok, ok,
+                                    parent.ctypes.data_as(C.c_void_p), ok, C.c_void_p(0), C.c_void_p(0), C.c_size_t(0), C.c_void_p(0)) == 1
