@@ -131,6 +131,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         n_splits = found[2];
         L = found[3];
         slot0 = found[4];
+        fence_proxy_async();  // (copies go to the same place next)
         __syncthreads();
         if (b < 0) return;  // (lengths that make fewer chunks than the host's)
     }
@@ -177,6 +178,7 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             }
         } else {
             for (int j = lane; j < C::BYTES / 4; j += 32) reinterpret_cast<uint32_t *>(mine + s * C::BYTES)[j] = 0x88888888u;
+            fence_proxy_async();  // (a later slice's copies go over them)
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
         }
