@@ -373,10 +373,13 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 at0 = at1;
                 --n_pend;
             };
-            auto next_k = [&](bool tree, int hkv, int at) {
+            auto next_k = [&](bool tree, int hkv, int at, auto &&ahead_of_v) {
                 post(tree ? TREE_K : TREE_K + 2, hkv, at, kp);
                 kp += kp < 2u ? 1u : 2u;
-                if (n_pend == 2) next_v();
+                if (n_pend == 2) {
+                    ahead_of_v();
+                    next_v();
+                }
                 const int kind = tree ? TREE_V : TREE_V + 2;
                 if (n_pend == 0) kind0 = kind, h0 = hkv, at0 = at;
                 else kind1 = kind, h1 = hkv, at1 = at;
@@ -423,7 +426,10 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                         tma_load_3d(q_s + qb * C::Q_BYTES + bx * BOX_BYTES, &tmQ, bx * 64, hkv * G,
                                     b * N + rb * a.nodes_per_block, bar(C::B_QFULL + qb));
                 };
-                // early cache loads, as below: the first unit's first pages go out before the kernel in front of this one has finished
+                // early cache loads, as below: the first unit's first pages go out before the kernel in front of this one has finished,
+                // but no more of them than there are slots (K0 K1 K2): the next job waits for a decoding team, which starts behind that
+                // kernel, and the time limit of such a wait is not to count that kernel's time
+                static_assert(C::SS >= 3, "three jobs that wait for nothing");
                 bool q_pending = early && u == 0;
                 auto settle = [&]() {
                     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -434,13 +440,12 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 int pg1 = n_kv > 1 ? __ldg(pt + 1) : 0;
                 for (int it = 0; it < n_kv && ok; ++it) {
                     const int pg2 = it + 2 < n_kv ? __ldg(pt + it + 2) : 0;
-                    if (q_pending && it >= 3) settle();
-                    next_k(false, hkv, pg);
+                    next_k(false, hkv, pg, [&]() { if (q_pending) settle(); });
                     pg = pg1;
                     pg1 = pg2;
                 }
                 if (q_pending) settle();
-                if (has_tree && ok) next_k(true, hkv, b * N);
+                if (has_tree && ok) next_k(true, hkv, b * N, []() {});
                 // (the unit's last V's follow the next unit's first K's.  Ahead of those, or with the next unit asked for before this one's last
                 // tile, they kept the teams from the tiles that were needed next: 204 us became 206 to 215 on 256 sequences, 56 rows.)
             }

@@ -1,5 +1,9 @@
 """The 4-bit paged cache where its kernels take other ways than small calls do: stages used again, many tokens, many layers, plans of many
 units.  Tables, bytes and copies exactly; attention with the tolerance of test_gpu_kv4.py."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -10,6 +14,8 @@ from tests.test_gpu_kv4 import _bits, _case, _check, _f64, _run
 from tests.util import dev, dev_bf16, host
 
 pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.mark.parametrize("N,Hq,D", [(1, 4, 64), (1, 16, 128), (8, 4, 128)])
@@ -27,3 +33,61 @@ def test_pages_that_are_missing_in_turn_with_pages_that_are_there(N, Hq, D, miss
                     w[b][at:at + 128] = 0
     O = _check(x)
     assert all(torch.equal(O, _run(x)) for _ in range(10))
+
+
+SETTLED = r"""
+import sys
+sys.path.insert(0, %r)
+import numpy as np, torch
+from paper_2608_04962_b200 import binding as S
+from tests.test_gpu_kv4 import _case, _run
+from tests.util import dev, dev_bf16
+assert S.check_status()[0] == 0, "not a build with index checks"
+g = torch.Generator(device="cuda").manual_seed(1)
+
+
+def long_call(Hkv, pages=900000, D=128):
+    pool = torch.randint(0, 255, (8, Hkv, 2, S.kv4_tile_bytes(D)), dtype=torch.uint8, device="cuda", generator=g)
+    table = torch.randint(0, 8, (pages,), dtype=torch.int32, device="cuda", generator=g)
+    lens = np.array([128 * pages - 5], np.int32)
+    Q, Kt, Vt = (torch.randn(1, 1, Hkv, D, device="cuda", generator=g).bfloat16() for _ in range(3))
+    ws = torch.zeros(S.tree_attn_kv4_workspace_bytes(1, 1, Hkv, Hkv, D, lens), dtype=torch.uint8, device="cuda")
+    indptr, on_gpu, out = torch.tensor([0, pages], dtype=torch.int32, device="cuda"), dev(lens), torch.empty_like(Q)
+    return lambda: S.tree_attn_kv4(Q, pool, table, indptr, on_gpu, lens, Kt, Vt, [-1], workspace=ws, out=out)
+
+
+def ms(f):
+    t = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    t[0].record()
+    f()
+    t[1].record()
+    torch.cuda.synchronize()
+    return t[0].elapsed_time(t[1])
+
+
+x = _case(4, 17, 4, 2, 128, [1000, 700, 1500, 384], seed=40)
+t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(x["len"]), x["len"], dev_bf16(x["Kt"]), dev_bf16(x["Vt"]), x["parent"]]
+ws, out = torch.zeros(S.tree_attn_kv4_workspace_bytes(4, 17, 4, 2, 128, x["len"]), dtype=torch.uint8, device="cuda"), torch.zeros_like(t[0])
+want = S.tree_attn_kv4(*t, workspace=ws).clone()
+even, uneven = long_call(98), long_call(100)
+even(), uneven()
+torch.cuda.synchronize()
+print("ms of 588 and of 600 units:", ms(even), ms(uneven))
+for _ in range(2):
+    out.zero_()
+    uneven()
+    S.tree_attn_kv4(*t, workspace=ws, out=out, flags=S.ATTN_REUSE_PLAN | S.ATTN_CACHE_SETTLED)
+    torch.cuda.synchronize()
+    assert S.workspace_status(ws) == 0 and torch.equal(out, want)
+print("settled ok")
+"""
+
+
+def test_a_settled_cache_behind_a_long_kernel():
+    """600 units where 592 run side by side: for tens of milliseconds few SMs are busy, and the next call's CTAs are there and fetch their
+    first pages.  The debug build's waits give up after 20 ms; none may be running by then."""
+    from paper_2608_04962_b200 import build as B
+    p = subprocess.run([sys.executable, "-c", SETTLED % ROOT], env=dict(os.environ, SPECROLL_LIB=B.build(check=True)), capture_output=True,
+                       text=True, timeout=600)
+    print(p.stdout)
+    assert p.returncode == 0 and "settled ok" in p.stdout, p.stdout + p.stderr
