@@ -326,7 +326,8 @@ def tree_attn_kv4(Q, pool, page_table, page_indptr, kv_len_dev, kv_len_host, Kt,
                   workspace=None, out=None, lse=None, flags: int = 0, check_status: bool = False):
     """specroll_tree_attn_kv4.  pool: uint8 [n_pages, Hkv, 2, kv4_tile_bytes(D)]; the other arguments as for
     ``tree_attn_paged``.  With N Hq / Hkv <= 16 the lengths on the device may be below ``kv_len_host`` (a call captured for the
-    longest, replayed as sequences grow).  Returns O (and lse when asked)."""
+    longest, replayed as sequences grow); if they need more than was planned for those, nothing is written and the status says so.
+    Returns O (and lse when asked)."""
     out, lse, workspace = _n().tree_attn_kv4(Q, pool, page_table, page_indptr, kv_len_dev, kv_len_host, Kt, Vt, parent, scale,
                                              want_lse, workspace, out, lse, flags)
     if check_status:

@@ -97,19 +97,29 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) own += i + q < b1 ? chunks(max(len[q], 0)) : 0;
+            own = min(own, a.items + 1);  // (sums stop there: what is beyond the host's chunks is too much, however far)
         }
         int sum = own;
 #pragma unroll
         for (int o_ = 1; o_ < 32; o_ <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, sum, o_);
-            if (lane >= o_) sum += x;
+            if (lane >= o_) sum = min(sum + x, a.items + 1);
         }
         if (lane == 31) found[8 + warp] = sum;
         if (threadIdx.x == 0) found[0] = -1;
         __syncthreads();
-        int at = sum - own;
+        const int ahead = __shfl_up_sync(0xffffffffu, sum, 1);
+        int at = lane ? ahead : 0, total = 0;
 #pragma unroll
-        for (int q = 0; q < WARPS - 1; ++q) at += q < warp ? found[8 + q] : 0;
+        for (int q = 0; q < WARPS; ++q) {
+            at += q < warp ? found[8 + q] : 0;
+            total += found[8 + q];
+        }
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            a.item_start[a.B] = total;  // (for the merge)
+            if (total > a.items) atomicExch(status, SPECROLL_ELIMIT);
+        }
+        if (total > a.items) return;  // lengths that make more chunks than the host's, which have no CTA and no place: nothing is written
         if (item >= at && item < at + own) {
             for (int i = b0; i < b1; ++i) {
                 const int len = max(__ldg(a.kv_len + i), 0), ns = chunks(len);
@@ -545,7 +555,7 @@ __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     pdl_wait();
     if (n_splits < 2) return;
     const int item0 = __ldcg(a.item_start + b);
-    if (item0 < 0 || item0 + n_splits > a.items) return;  // (lengths that are not the host's)
+    if (__ldcg(a.item_start + a.B) > a.items) return;  // (lengths that make more chunks than the host's: the attention kernel has said so)
     const size_t unit = (size_t)item0 * a.Hkv + hkv;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + unit * a.rows_pad + row;
     const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + (unit * (D / 4) + d4) * a.rows_pad + row;

@@ -91,3 +91,42 @@ def test_a_settled_cache_behind_a_long_kernel():
                        text=True, timeout=600)
     print(p.stdout)
     assert p.returncode == 0 and "settled ok" in p.stdout, p.stdout + p.stderr
+
+
+@pytest.mark.parametrize("N,Hq,host_lens", [(1, 4, [3000, 200, 100, 2000]), (8, 4, [2000, 200, 2500, 100]), (1, 32, [4000, 0, 0, 0])])
+@pytest.mark.parametrize("D", [64, 128])
+def test_lengths_above_the_hosts_are_reported_and_nothing_is_written(N, Hq, host_lens, D):
+    """A cut plan of few rows, replayed on lengths that make more chunks than it has: the status word says so, and outputs stay as they were,
+    whatever an earlier call has left in the workspace."""
+    x = _case(4, N, Hq, 2, D, [9000, 8000, 7000, 9100], seed=50)
+    host_lens = np.array(host_lens, np.int32)
+    ws = S.alloc(S.tree_attn_kv4_workspace_bytes(4, N, Hq, 2, D, host_lens), dtype=torch.uint8, device="cuda")
+    t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(host_lens), host_lens, dev_bf16(x["Kt"]), dev_bf16(x["Vt"])]
+    out = [torch.empty_like(t[0]), torch.empty(t[0].shape[:3], device="cuda")]
+
+    def call():
+        S.tree_attn_kv4(*t, x["parent"], workspace=ws, out=out[0], lse=out[1])
+        return [o.clone() for o in out]
+    want = call()
+    assert S.workspace_status(ws) == 0
+    short = {**x, "len": host_lens, "K": [k[:n] for k, n in zip(x["K"], host_lens)], "V": [v[:n] for v, n in zip(x["V"], host_lens)]}
+    assert torch.equal(want[0], _check(short))
+    for lens in (x["len"], np.where(np.arange(4) == 3, x["len"], host_lens), np.where(np.arange(4) == 1, x["len"], host_lens),
+                 host_lens + [300, 9000, 0, 0]):
+        t[4].copy_(dev(np.minimum(lens, x["len"]).astype(np.int32)))
+        for o in out:
+            o.fill_(-7.0)
+        assert all(bool((o == -7.0).all()) for o in call()) and S.workspace_status(ws) == 6
+        with pytest.raises(S.SpecrollError):
+            S.tree_attn_kv4(*t, x["parent"], workspace=ws, out=out[0], lse=out[1], check_status=True)
+        t[4].copy_(dev(host_lens))
+        assert all(torch.equal(o, w) for o, w in zip(call(), want)) and S.workspace_status(ws) == 0
+
+
+def test_a_few_tokens_above_the_hosts_lengths():
+    """More tokens, but no more chunks than the host's lengths make, or nothing cut at all: the lengths on the device are followed."""
+    for lens, above in (([9000, 300], [9001, 330]), ([100, 120, 64], [129, 600, 0])):
+        x = _case(len(lens), 1, 4, 2, 128, above, seed=51)
+        t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(x["len"]), np.array(lens, np.int32), dev_bf16(x["Kt"]), dev_bf16(x["Vt"])]
+        got, want = S.tree_attn_kv4(*t, x["parent"], check_status=True), _check(x)
+        assert (got.float() - want.float()).abs().max() <= 2.0 ** -6 * want.float().abs().max()
