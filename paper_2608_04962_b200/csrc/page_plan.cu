@@ -51,7 +51,8 @@ page_plan_kernel(const PagePlanArgs a) {
     const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS, b0 = min(B, t * per), b1 = min(B, b0 + per);
     auto of_seq = [&](int b, int add, uint32_t (&v)[4]) {
         const uint32_t had = (uint32_t)hads[b], more = add < 0 ? 0u : (uint32_t)add;
-        const uint32_t need = ((uint32_t)lens[b] + more + (SPECROLL_PAGE_TOKENS - 1)) / SPECROLL_PAGE_TOKENS;  // (below 2^32: both are below 2^31)
+        // (in 64 bits: both are below 2^31, but their sum rounded up to pages may pass 2^32)
+        const uint32_t need = (uint32_t)(((unsigned long long)(uint32_t)lens[b] + more + (SPECROLL_PAGE_TOKENS - 1)) / SPECROLL_PAGE_TOKENS);
         v[1] = more;
         v[2] = add < 0 || need < had ? 0u : need - had;
         v[0] = add < 0 ? 0u : had + v[2];

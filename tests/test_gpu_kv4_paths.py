@@ -130,3 +130,16 @@ def test_a_few_tokens_above_the_hosts_lengths():
         t = [dev_bf16(x["Q"]), dev(x["pool"]), dev(x["table"]), dev(x["indptr"]), dev(x["len"]), np.array(lens, np.int32), dev_bf16(x["Kt"]), dev_bf16(x["Vt"])]
         got, want = S.tree_attn_kv4(*t, x["parent"], check_status=True), _check(x)
         assert (got.float() - want.float()).abs().max() <= 2.0 ** -6 * want.float().abs().max()
+
+
+@pytest.mark.parametrize("kv_len,add", [(2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 31 - 126), (2 ** 31 - 130, 5), (0, 2 ** 31 - 1), (2 ** 31 - 1, 0)])
+def test_a_page_plan_of_the_longest_lengths(kv_len, add):
+    """The pages that a length near 2^31 needs, also where it and the tokens to come round up past 2^32."""
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = ([kv_len, 100], [add, 100], [7, 8, 9], [0, 2, 3], [4, 2, 5, 0], [3])
+    p = S.page_plan(*[dev(np.array(a, np.int32)) for a in args], 8, 6, status=status)
+    need = -(-(kv_len + add) // 128)
+    assert host(p["page_indptr"]).tolist() == [0, need, need + 2]
+    assert host(p["tok_indptr"]).tolist() == [0, add, min(add + 100, 2 ** 31 - 1)]
+    assert host(p["page_table"]).tolist() == [7, 8, 4, 2, 5, -1, -1, -1]     # (all there are; the second sequence's places are far beyond)
+    assert int(p["n_free"]) == 0 and host(p["free_list"]).tolist() == [-1] * 4 and int(status) == 6
