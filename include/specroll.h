@@ -274,8 +274,9 @@ int specroll_gather_hidden(int32_t B, int32_t N, int32_t d, const void *hidden,
  * Outputs: page_table_out[table_cap] and page_indptr_out[B + 1], the new tables; tok_indptr[B + 1] and slot_map[slot_cap], where
  * slot_map[tok_indptr[b] + i] = page * 128 + place is the slot of position kv_len[b] + i, i < add[b], as
  * specroll_kv4_store takes it; free_list_out[free_cap] and *n_free_out.  Entries behind the last one are -1 in all three arrays,
- * and so are pages that the free list did not have and the slots on them.  When it runs out, or an array is too short (what does
- * not fit is not written), *status (device word, nullable; never cleared here) becomes SPECROLL_ELIMIT; the state to go on from is
+ * and so are pages that the free list did not have and the slots on them.  When it runs out, an array is too short (what does
+ * not fit is not written), or a sequence's places page_indptr[b] .. page_indptr[b + 1] decrease or do not all lie in page_table (those outside
+ * count as pages -1), *status (device word, nullable; never cleared here) becomes SPECROLL_ELIMIT; the state to go on from is
  * then the old one (a page -1 in a table is a page like any other here: it would go back to the free list).
  * n_table: entries of page_table (it is not read beyond them).  Outputs must not overlap inputs or one another.
  * All pointers device; slot_map i64 and 16-byte aligned, the others i32; B <= 4096 (else SPECROLL_ELIMIT), free_cap <= 2^24.

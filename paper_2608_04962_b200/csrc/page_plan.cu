@@ -59,15 +59,18 @@ page_plan_kernel(const PagePlanArgs a) {
         v[3] = add < 0 ? had : 0u;
     };
     uint32_t run[4] = {0u, 0u, 0u, 0u}, tot[4], one[4];
+    bool astray = false;  // a sequence whose pages are not all in the table: those outside count as -1, and the caller is told
     for (int b = b0; b < b1; ++b) {
         const int at = a.indptr[b], end = a.indptr[b + 1], add = a.add[b], len = a.kv_len[b];
         old_at[b] = at;
-        hads[b] = max(end - at, 0);
+        hads[b] = end > at ? (int)min((long long)end - at, (long long)PLAN_SAT) : 0;
+        astray |= end < at || (end > at && (at < 0 || end > a.n_table));
         lens[b] = max(len, 0);
         of_seq(b, add, one);
 #pragma unroll
         for (int q = 0; q < 4; ++q) run[q] = plan_add(run[q], one[q]);
     }
+    if (astray && blockIdx.x == 0 && a.status) atomicExch(a.status, SPECROLL_ELIMIT);
     uint32_t before[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {

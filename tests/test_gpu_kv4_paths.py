@@ -143,3 +143,29 @@ def test_a_page_plan_of_the_longest_lengths(kv_len, add):
     assert host(p["tok_indptr"]).tolist() == [0, add, min(add + 100, 2 ** 31 - 1)]
     assert host(p["page_table"]).tolist() == [7, 8, 4, 2, 5, -1, -1, -1]     # (all there are; the second sequence's places are far beyond)
     assert int(p["n_free"]) == 0 and host(p["free_list"]).tolist() == [-1] * 4 and int(status) == 6
+
+
+@pytest.mark.parametrize("indptr,status_is", [([0, 2, 3, 5], 0), ([1, 2, 2, 5], 0), ([0, 2, 3, 6], 6), ([0, 2, 7, 9], 6), ([-1, 2, 3, 5], 6),
+                                              ([0, 3, 2, 5], 6), ([0, 0, 0, 0], 0), ([9, 9, 9, 9], 0), ([-2 ** 31, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1], 6)])
+@pytest.mark.parametrize("add", [(1, 1, 1), (1, -1, 1), (-1, -1, -1)])
+def test_a_page_plan_of_places_outside_the_table(indptr, status_is, add):
+    """A sequence whose places are not all in the table is reported, live or finished; what lies inside is what it was."""
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    table = np.array([10, 11, 12, 13, 14], np.int32)
+    args = [np.array(a, np.int32) for a in ([0, 0, 0], add, table, indptr, [4, 2, 5, 3] + [0] * 12, [4])]
+    p = S.page_plan(*[dev(a) for a in args], 16, 3, status=status)
+    assert int(status) == status_is
+    if status_is == 0:
+        want = ref.page_plan(*args[:5], 4, 16, 3)
+        for k in ("page_table", "page_indptr", "tok_indptr", "slot_map", "free_list"):
+            assert np.array_equal(host(p[k]), want[k]), k
+    elif indptr[0] >= -1:
+        own = [[int(table[i]) if 0 <= i < 5 else -1 for i in range(indptr[b], indptr[b + 1])] for b in range(3)]
+        free, tables = [4, 2, 5, 3], []
+        for b in range(3):
+            tables.append([] if add[b] < 0 else own[b] or [free.pop(0)])
+        for b in range(3):
+            free += own[b] if add[b] < 0 else []
+        flat = sum(tables, [])
+        assert host(p["page_table"]).tolist() == flat + [-1] * (16 - len(flat))
+        assert host(p["free_list"]).tolist() == free + [-1] * (16 - len(free)) and int(p["n_free"]) == len(free)
