@@ -308,12 +308,13 @@ int specroll_kv4_store(int64_t T, int32_t Hkv, int32_t D, const void *K, const v
                        int64_t n_pages, int32_t *status, void *cuda_stream);
 
 /* The values at the slots slot_map[T] back as bf16 K, V[T, Hkv, D] (exactly; a slot may occur more than once): a cached prefix for
- * kernels that read bf16, or a cache on its way out.  Zeros for slots that are negative or beyond the pool; *status as above. */
+ * kernels that read bf16, or a cache on its way out.  Zeros for slots that are negative or beyond the pool; *status as above.  K and V
+ * must not overlap (SPECROLL_EINVAL). */
 int specroll_kv4_load(int64_t T, int32_t Hkv, int32_t D, const void *pool, int64_t n_pages, const int64_t *slot_map, void *K,
                       void *V, int32_t *status, void *cuda_stream);
 
-/* specroll_commit_path and specroll_commit_path_layers for pools in 4 bits (pool: one per layer in the place of Kp and Vp); everything
- * else as there. */
+/* specroll_commit_path and specroll_commit_path_layers for pools in 4 bits (pool: one per layer in the place of Kp and Vp, all different);
+ * everything else as there. */
 int specroll_commit_path_kv4(int32_t B, int32_t N, int32_t K, int32_t Hkv, int32_t D, const void *Kt, const void *Vt,
                              const int32_t *path_node, const int32_t *n_acc, void *pool, int64_t n_pages,
                              const int32_t *page_table, const int32_t *page_indptr, const int32_t *kv_len,

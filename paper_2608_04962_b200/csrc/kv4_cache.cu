@@ -310,6 +310,9 @@ extern "C" int specroll_kv4_load(int64_t T, int32_t Hkv, int32_t D, const void *
     dim3 grid;
     const int rc = by_slot(T, Hkv, D, K, V, slot_map, pool, n_pages, &a, &grid);
     if (rc != SPECROLL_OK || grid.x == 0) return rc;
+    // (two threads would write one place: which value stays would be a matter of luck)
+    const uintptr_t k = reinterpret_cast<uintptr_t>(K), v = reinterpret_cast<uintptr_t>(V), bytes = (uintptr_t)T * a.columns * 8;
+    if (k < v + bytes && v < k + bytes) return SPECROLL_EINVAL;
     SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_load_kernel<128> : kv4_load_kernel<64>, grid, dim3(KV4_THREADS), 0,
                                  static_cast<cudaStream_t>(cuda_stream), static_cast<const uint8_t *>(pool), a, static_cast<uint4 *>(K),
                                  static_cast<uint4 *>(V), status));

@@ -148,3 +148,11 @@ def test_lengths_that_round_up_past_31_bits_are_refused(N, Hq, Hkv):
     L = S.lib()
     assert L.specroll_tree_attn_kv4(C.byref(d), ok, ok, C.c_int64(4), ok, ok, ok, lens.ctypes.data_as(C.c_void_p), ok, ok,
                                     parent.ctypes.data_as(C.c_void_p), ok, C.c_void_p(0), C.c_void_p(0), C.c_size_t(0), C.c_void_p(0)) == 1
+
+
+def test_loading_k_and_v_to_one_place_is_refused():
+    L, null, _ = _null_calls()
+    base, i32, i64 = np.zeros(64, np.int64).ctypes.data // 16 * 16 + 16, C.c_int32, C.c_int64
+    at = lambda off: C.c_void_p(base + off)  # noqa: E731
+    for off in (0, 16, 4 * 2 * 64 * 2 - 16, -16, 16 - 4 * 2 * 64 * 2):         # (never read or written: refused on the host)
+        assert L.specroll_kv4_load(i64(4), i32(2), i32(64), at(0), i64(1), at(0), at(0), at(off), null, null) == 1
