@@ -169,3 +169,126 @@ def test_a_page_plan_of_places_outside_the_table(indptr, status_is, add):
         flat = sum(tables, [])
         assert host(p["page_table"]).tolist() == flat + [-1] * (16 - len(flat))
         assert host(p["free_list"]).tolist() == free + [-1] * (16 - len(free)) and int(p["n_free"]) == len(free)
+
+
+# ------------------------------------------------------------------ writers and reader of many tokens and layers
+
+def _stored(pool, slots, K, V, D):
+    """The pool after K, V [T, Hkv, D] (float64) have gone to slots that differ (negative ones: nowhere), all tokens at once."""
+    q, c = (x.copy() for x in ref.kv4_unpack(pool, D))                       # [page, Hkv, K or V, 128, ..]
+    on = slots >= 0
+    page, at = np.divmod(slots[on], 128)
+    for i, x in enumerate((K, V)):
+        xq, xc = ref.kv4_quantise(x[on])
+        q[page, :, i, at], c[page, :, i, at] = xq, xc
+    return ref.kv4_pack(q, c)
+
+
+def test_the_oracle_for_many_tokens_is_the_oracle():
+    g = np.random.default_rng(1)
+    pool = g.integers(0, 256, (3, 2, 2, S.kv4_tile_bytes(64))).astype(np.uint8)
+    slots, K, V = g.permutation(384)[:50].astype(np.int64), *(_f64(_bits(g, 50, 2, 64)) for _ in range(2))
+    slots[3] = -1
+    assert np.array_equal(_stored(pool, slots, K, V, 64), ref.kv4_store(K, V, slots, pool))
+
+
+@pytest.mark.parametrize("T,H,D", [(1301, 8, 128), (9601, 2, 64), (6403, 3, 64), (803, 12, 128), (37, 12, 128), (130, 33, 64), (18949, 1, 64),
+                                   (1185, 8, 128), (1184, 8, 128)])
+def test_store_and_load_of_many_tokens_and_of_many_heads(T, H, D):
+    """Four tokens a thread and a remainder (more than 303104 words of eight elements in all), tokens side by side in a block or a token in
+    several blocks, and the largest call with one token a thread."""
+    g = np.random.default_rng(T)
+    K, V = _bits(g, T, H, D), _bits(g, T, H, D)
+    pages = T // 128 + 2
+    pool = g.integers(0, 256, (pages, H, 2, S.kv4_tile_bytes(D))).astype(np.uint8)
+    slots = g.permutation(pages * 128)[:T].astype(np.int64)
+    slots[g.permutation(T)[:5]] = -1
+    dpool, status = dev(pool), torch.zeros(1, dtype=torch.int32, device="cuda")
+    S.kv4_store(dev_bf16(K), dev_bf16(V), dev(slots), dpool, status=status)
+    assert np.array_equal(host(dpool), _stored(pool, slots, _f64(K), _f64(V), D))
+    for got, x in zip(S.kv4_load(dpool, dev(slots), status=status), (K, V)):
+        want = np.where((slots >= 0)[:, None, None], ref.kv4_values(*ref.kv4_quantise(_f64(x))), 0.0)
+        assert np.array_equal(host(got.double()), want)
+    assert int(status) == 0
+    far = slots.copy()
+    far[T - 1] = pages * 128                                                 # the last token's slot is beyond the pool: only that is told
+    S.kv4_store(dev_bf16(K), dev_bf16(V), dev(far), dpool, status=status)
+    assert int(status) == 6
+
+
+@pytest.mark.parametrize("B,layers,H,D,N,K", [(48, 28, 2, 64, 16, 4), (200, 27, 1, 64, 8, 5), (20, 65, 2, 128, 9, 8), (150, 9, 12, 128, 6, 2), (3, 130, 1, 64, 4, 1),
+                                              (70, 17, 3, 128, 30, 7), (301, 8, 8, 128, 5, 3)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_commit_of_many_layers(B, layers, H, D, N, K, in_place):
+    """Up to eight layers to a block with a remainder, rows of more than 256 words, and more layers than one launch takes."""
+    g = np.random.default_rng(B + layers)
+    kv_len = g.integers(0, 300, B).astype(np.int32)
+    own = (kv_len + K + 1 + 127) // 128
+    indptr = np.concatenate([[0], np.cumsum(own)]).astype(np.int32)
+    table = g.permutation(indptr[-1] + 2)[:indptr[-1]].astype(np.int32)
+    n_acc = g.integers(-1, min(K, N - 1) + 1, B).astype(np.int32)
+    path = np.sort(np.argsort(g.random((B, max(N, K + 1))), 1)[:, :K + 1], 1).astype(np.int32) % N
+    pos = kv_len[:, None] + np.arange(K + 1)
+    slots = table[indptr[:-1, None] + pos // 128].astype(np.int64) * 128 + pos % 128
+    slots[np.arange(K + 1) > n_acc[:, None]] = -1
+    gt = torch.Generator(device="cuda").manual_seed(B)
+    Kt, Vt = (torch.randn(layers, B, N, H, D, device="cuda", generator=gt).bfloat16() for _ in range(2))
+    pools = torch.randint(0, 256, (layers, int(indptr[-1]) + 2, H, 2, S.kv4_tile_bytes(D)), dtype=torch.uint8, device="cuda", generator=gt)
+    before = pools.clone()
+    status, lens = torch.zeros(1, dtype=torch.int32, device="cuda"), dev(kv_len)
+    out = lens if in_place else torch.full_like(lens, -9)
+    S.commit_path_kv4_layers(list(Kt), list(Vt), dev(path), dev(n_acc), list(pools), dev(table), dev(indptr), lens, kv_len_out=out, status=status)
+    assert int(status) == 0 and np.array_equal(host(out), kv_len + n_acc + 1)
+    seq = torch.arange(B, device="cuda")[:, None]
+    for l in range(layers):                                                  # (every layer against the writer by slot, some against the oracle)
+        rows = [x[l][seq, dev(path).long()].flatten(0, 1).contiguous() for x in (Kt, Vt)]
+        want = before[l].clone()
+        S.kv4_store(*rows, dev(slots.reshape(-1)), want)
+        assert torch.equal(pools[l], want), l
+    for l in {0, layers // 2, layers - 1}:
+        rows = [host(x[l][seq, dev(path).long()].flatten(0, 1).double()) for x in (Kt, Vt)]
+        assert np.array_equal(host(pools[l]), _stored(host(before[l]), slots.reshape(-1), *rows, D)), l
+
+
+# ------------------------------------------------------------------ plans of many units
+
+def _cut(x):
+    """Whether the plan cuts a sequence (its workspace is then larger than that of as many sequences of one token)."""
+    B, N, Hq, D = x["Q"].shape
+    f = S.tree_attn_kv4_workspace_bytes
+    return f(B, N, Hq, x["Kt"].shape[2], D, x["len"]) > f(B, N, Hq, x["Kt"].shape[2], D, np.ones(B, np.int32))
+
+
+@pytest.mark.parametrize("N,Hq,Hkv,D,lengths,merged_inside", [
+    (17, 4, 4, 128, [2100] + [300 + 7 * b for b in range(39)], True), (24, 14, 2, 128, [2000, 1900] + [b * 53 % 700 for b in range(100)], True),
+    (48, 10, 2, 128, [1500, 1400] + [b * 11 % 700 for b in range(60)], True), (33, 4, 4, 64, [1500, 1400] + [b * 53 % 700 for b in range(60)], True),
+    (20, 6, 2, 128, [(b * 53) % 400 for b in range(180)], False), (18, 1, 1, 64, [(b * 31) % 300 for b in range(700)], False)])
+def test_trees_in_more_units_than_ctas(N, Hq, Hkv, D, lengths, merged_inside):
+    """Persistent CTAs that take several units each, with sequences in two to four chunks that the attention kernel merges itself, or whole."""
+    x = _case(len(lengths), N, Hq, Hkv, D, lengths, seed=N)
+    indptr = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    assert _cut(x) == merged_inside and S.tree_attn_launches(len(lengths), N, Hq, Hkv, D, indptr) == 2   # (plan and attention: no kernel merges)
+    O = _check(x)
+    assert all(torch.equal(O, _run(x)) for _ in range(10))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N,Hq,Hkv,lengths", [(2, 8, 1, [9000]), (1, 8, 1, [9000, 0, 1]), (1, 16, 1, [700, 9001, 130]), (16, 1, 1, [5000, 4999])])
+def test_few_rows_in_many_chunks(N, Hq, Hkv, lengths, D):
+    """More than eight chunks of a sequence: the merge with several blocks a sequence and head, for both numbers of rows and both widths."""
+    x = _case(len(lengths), N, Hq, Hkv, D, lengths, seed=60)
+    assert _cut(x)
+    O = _check(x)
+    assert all(torch.equal(O, _run(x)) for _ in range(10))
+
+
+@pytest.mark.parametrize("N,Hq", [(1, 4), (3, 4)])
+def test_few_rows_of_many_sequences_of_which_some_are_cut(N, Hq):
+    """The search for a unit where a thread has more sequences than it keeps pages of."""
+    lengths = [(b * 13) % 90 for b in range(700)]
+    for b in (0, 3, 5, 411, 699):
+        lengths[b] = 20000 + b
+    x = _case(700, N, Hq, 1, 64, lengths, seed=61)
+    assert _cut(x)
+    O = _check(x)
+    assert all(torch.equal(O, _run(x)) for _ in range(10))
