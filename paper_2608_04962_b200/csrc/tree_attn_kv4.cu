@@ -42,7 +42,8 @@ struct Cfg {
     static constexpr int O_FLOATS = D * ROWS;
     static constexpr int JOIN = WARPS * (O_FLOATS + 2 * ROWS) * 4;
     static constexpr int BODY = (RING > JOIN ? RING : JOIN);
-    static constexpr int SMEM = BODY + 8 * WARPS * STAGES + 16;
+    static constexpr int FOUND = BODY + 8 * WARPS * STAGES + 16;  // the unit's search
+    static constexpr int SMEM = FOUND + 4 * (8 + WARPS);
     static constexpr int CTAS = R8 == 1 ? KV4_CTAS_8 : KV4_CTAS_16;
     static_assert(SCALES % 16 == 0 && CTAS * (SMEM + 1024) <= 233472, "bulk copies; shared memory of an SM");
 };
@@ -82,7 +83,9 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         L = max(__ldg(a.kv_len + b), 0);
         slot0 = __ldg(a.page_indptr + b);
     } else {
-        volatile int *const found = reinterpret_cast<volatile int *>(smem);  // [0..5]: the unit, [8 ..]: chunks of the warps' sequences
+        // [0..4]: the unit, [8 ..]: chunks of the warps' sequences.  (Not in the ring: copies go there next, which would take a fence
+        // and a barrier.)
+        volatile int *const found = reinterpret_cast<volatile int *>(smem + C::FOUND);
         const int per = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
         auto chunks = [&](int len) { return max(1, ((len + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS + a.chunk_tiles - 1) / a.chunk_tiles); };
         // (lengths four at a time, so that their loads are under way together; the first four sequences' pages as well)
@@ -97,29 +100,30 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) own += i + q < b1 ? chunks(max(len[q], 0)) : 0;
-            own = min(own, a.items + 1);  // (sums stop there: what is beyond the host's chunks is too much, however far)
+            own = min(own, a.items + 1);  // (what is beyond the host's chunks is too much, however far; those are some thousands at most)
         }
         int sum = own;
 #pragma unroll
         for (int o_ = 1; o_ < 32; o_ <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, sum, o_);
-            if (lane >= o_) sum = min(sum + x, a.items + 1);
+            if (lane >= o_) sum += x;
         }
         if (lane == 31) found[8 + warp] = sum;
         if (threadIdx.x == 0) found[0] = -1;
         __syncthreads();
-        const int ahead = __shfl_up_sync(0xffffffffu, sum, 1);
-        int at = lane ? ahead : 0, total = 0;
+        int at = sum - own, total = 0;
 #pragma unroll
         for (int q = 0; q < WARPS; ++q) {
             at += q < warp ? found[8 + q] : 0;
             total += found[8 + q];
         }
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            a.item_start[a.B] = total;  // (for the merge)
-            if (total > a.items) atomicExch(status, SPECROLL_ELIMIT);
+        if (total > a.items) {  // lengths that make more chunks than the host's, which have no CTA and no place: nothing is written
+            if (blockIdx.x == 0) {
+                for (int i = b0; i < b1; ++i) a.item_start[i] = a.items;  // (the merge sees by it that its sequence has no chunks)
+                if (threadIdx.x == 0) atomicExch(status, SPECROLL_ELIMIT);
+            }
+            return;
         }
-        if (total > a.items) return;  // lengths that make more chunks than the host's, which have no CTA and no place: nothing is written
         if (item >= at && item < at + own) {
             for (int i = b0; i < b1; ++i) {
                 const int len = max(__ldg(a.kv_len + i), 0), ns = chunks(len);
@@ -141,8 +145,6 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         n_splits = found[2];
         L = found[3];
         slot0 = found[4];
-        fence_proxy_async();  // (copies go to the same place next)
-        __syncthreads();
         if (b < 0) return;  // (lengths that make fewer chunks than the host's)
     }
     const int tiles_b = (L + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS;
@@ -555,7 +557,7 @@ __global__ void __launch_bounds__(256) attn_merge_kv4_kernel(AttnArgs a) {
     pdl_wait();
     if (n_splits < 2) return;
     const int item0 = __ldcg(a.item_start + b);
-    if (__ldcg(a.item_start + a.B) > a.items) return;  // (lengths that make more chunks than the host's: the attention kernel has said so)
+    if (item0 + n_splits > a.items) return;  // (lengths that make more chunks than the host's: the attention kernel has said so)
     const size_t unit = (size_t)item0 * a.Hkv + hkv;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + unit * a.rows_pad + row;
     const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + (unit * (D / 4) + d4) * a.rows_pad + row;
