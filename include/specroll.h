@@ -331,8 +331,9 @@ int specroll_commit_path_kv4_layers(int32_t B, int32_t N, int32_t K, int32_t Hkv
  * token a sequence, whose own K and V are Kt and Vt.  Tree rows that a node does not see are multiplied by a zero weight: they must hold
  * finite values.  Pages outside [0, n_pages) read as zeros.  Flags, plan and workspace as for specroll_tree_attn_paged.
  * With up to 16 query rows (N Hq / Hkv) per KV head the lengths on the device may be below the host's, so that a call captured for the
- * longest that the sequences get can be replayed as they grow; lengths above the host's that make more chunks of pages than those leave O
- * and lse as they were and the workspace's status word at SPECROLL_ELIMIT.  With more rows both copies have the same values, in replays too. */
+ * longest that the sequences get can be replayed as they grow.  Lengths above the host's are followed as long as the sequences need no more
+ * chunks of pages than were planned for those (or none was cut); else O and lse stay as they were and the workspace's status word becomes
+ * SPECROLL_ELIMIT.  With more rows both copies have the same values, in replays too. */
 size_t specroll_tree_attn_kv4_workspace_bytes(const specroll_attn_desc *desc, const int32_t *kv_len_host);
 
 int specroll_tree_attn_kv4(const specroll_attn_desc *desc, const void *Q, const void *pool, int64_t n_pages,

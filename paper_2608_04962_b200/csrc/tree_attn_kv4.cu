@@ -87,7 +87,9 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         // and a barrier.)
         volatile int *const found = reinterpret_cast<volatile int *>(smem + C::FOUND);
         const int per = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
-        auto chunks = [&](int len) { return max(1, ((len + SPECROLL_PAGE_TOKENS - 1) / SPECROLL_PAGE_TOKENS + a.chunk_tiles - 1) / a.chunk_tiles); };
+        auto chunks = [&](int len) {  // (the rounding without a sign: the longest lengths pass 31 bits by it)
+            return max(1, ((int)(((unsigned)len + (SPECROLL_PAGE_TOKENS - 1)) / SPECROLL_PAGE_TOKENS) + a.chunk_tiles - 1) / a.chunk_tiles);
+        };
         // (lengths four at a time, so that their loads are under way together; the first four sequences' pages as well)
         int own = 0, pages[4];
         for (int i = b0; i < b1; i += 4) {

@@ -112,8 +112,8 @@ def test_lengths_above_the_hosts_are_reported_and_nothing_is_written(N, Hq, host
     short = {**x, "len": host_lens, "K": [k[:n] for k, n in zip(x["K"], host_lens)], "V": [v[:n] for v, n in zip(x["V"], host_lens)]}
     assert torch.equal(want[0], _check(short))
     for lens in (x["len"], np.where(np.arange(4) == 3, x["len"], host_lens), np.where(np.arange(4) == 1, x["len"], host_lens),
-                 host_lens + [300, 9000, 0, 0]):
-        t[4].copy_(dev(np.minimum(lens, x["len"]).astype(np.int32)))
+                 host_lens + [300, 9000, 0, 0], np.where(np.arange(4) == 2, 2 ** 31 - 1, host_lens), np.full(4, 2 ** 31 - 20)):
+        t[4].copy_(dev((lens if lens.max() > 2 ** 30 else np.minimum(lens, x["len"])).astype(np.int32)))   # (nothing is read of the longest)
         for o in out:
             o.fill_(-7.0)
         assert all(bool((o == -7.0).all()) for o in call()) and S.workspace_status(ws) == 6
