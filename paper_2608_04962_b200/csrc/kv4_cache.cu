@@ -345,7 +345,7 @@ extern "C" int specroll_commit_path_kv4_layers(int32_t B, int32_t N, int32_t K, 
             lay.Vt[l] = static_cast<const uint4 *>(Vt[l0 + l]);
             lay.pool[l] = static_cast<uint8_t *>(pool[l0 + l]);
         }
-        // layers to a block: as many as leave four blocks to every SM, up to 8 (256 sequences, 28 layers of two heads, us: 27.4 with two
+        // layers to a block: as many as leave four blocks to every SM, up to 8 (256 sequences, 28 layers of two heads, with all rows read back, us: 27.4 with two
         // layers, 22.4 with four, 20.3 with eight, 21.1 with twelve, 28.5 with all)
         const int each = (int)std::min<long long>(std::max<long long>((long long)B * nl / (4LL * n_sm), 1), 8);
         SR_CUDA_TRY(launch_dependent(true, D == 128 ? kv4_commit_kernel<128> : kv4_commit_kernel<64>,

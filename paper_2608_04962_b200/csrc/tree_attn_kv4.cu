@@ -14,7 +14,7 @@
 // shared memory at the end.  The tree's bf16 rows (sixteen nodes at most) are done by the first warp before its slices.
 // What bounds it: long sequences take an SM 0.50 us a page and head (17 KB, 0.39 at HBM's rate: 79 %; without decoding 0.42).  Decoding
 // is some 80 integer and 64 packed floating operations a thread for 16 tokens, which the tensor operations and the rest do not quite hide;
-// more warps on an SM (five CTAs at 96 registers) changed nothing, nor did whole pages by one copy each into stages that the four
+// more warps on an SM (five CTAs at 96 registers; there are 128, with 28 bytes of spill where D = 128) changed nothing, nor did whole pages by one copy each into stages that the four
 // warps share.  A unit takes 12 us beyond its pages: lengths, page table, pages, then the warps' meeting, each a round trip, of which
 // the other three CTAs of the SM hide a part.
 #include <math.h>
@@ -322,6 +322,8 @@ tree_attn_kv4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 l[r][1] += sum[r][1];
 #pragma unroll
                 for (int p = 0; p < GP; ++p) {
+                    // (bf16, the type of V in the product: half a step is 2^-8 of each, outputs are 2.3e-3 from 64 bits, of which their own
+                    // rounding is 1.7e-3; the sums above are of the probabilities in fp32)
                     pf[p][r][0] = movmatrix(pack_bf16x2(q[p][r][0] * down, q[p][r][1] * down));
                     pf[p][r][1] = movmatrix(pack_bf16x2(q[p][r][2] * down, q[p][r][3] * down));
                 }

@@ -987,6 +987,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                                 const float p1 = b1 ? ex2_approx(fmaf(__uint_as_float(src[i2 + 1]), sct, -mref_)) : 0.f;
                                 ls0 += p0;
                                 ls1 += p1;
+                                // (bf16, the type of V in the product: half a step is 2^-8 of each; the sums above are fp32)
                                 pk[i2 >> 1] = KV4 ? pack_bf16x2(p0 * down, p1 * down) : pack_bf16x2(p0, p1);
                             }
                         }
@@ -1546,7 +1547,8 @@ int launch_attn_merge_tc(const AttnArgs &a, int D, int items, int max_splits, cu
 
 int launch_attn_tc(const AttnArgs &a, const TopoMask &mask, int D, long long T_kv, int32_t *status, cudaStream_t st) {
     // One row block per (sequence, KV head): the kernel is bound by HBM and the softmax with two threads per row
-    // is (slightly) the better one; more blocks: bound by the softmax, where the two alternating teams are faster.
+    // is (slightly) the better one; more blocks: bound by the softmax, where the two alternating teams are faster.  (Over a 4-bit
+    // cache nothing is bound by HBM, and only the form with two teams was built.)
     const bool teams = a.n_rb > 1;
     if (a.kv4) return D == 128 ? launch_tc<128, true, true>(a, mask, T_kv, status, st) : launch_tc<64, true, true>(a, mask, T_kv, status, st);
     if (D == 128) return teams ? launch_tc<128, true, false>(a, mask, T_kv, status, st) : launch_tc<128, false, false>(a, mask, T_kv, status, st);
