@@ -329,7 +329,8 @@ int specroll_commit_path_kv4_layers(int32_t B, int32_t N, int32_t K, int32_t Hkv
 /* specroll_tree_attn_paged over such a pool: exactly the attention of the cached values as decoded and of the tree's bf16 rows Kt, Vt
  * (scores and sums in fp32, probabilities rounded to bf16 for the product with V, as there).  N = 1 with parent {-1} is plain decoding of one
  * token a sequence, whose own K and V are Kt and Vt.  Tree rows that a node does not see are multiplied by a zero weight: they must hold
- * finite values.  Pages outside [0, n_pages) read as zeros.  Flags, plan and workspace as for specroll_tree_attn_paged.
+ * finite values.  Pages outside [0, n_pages) read as zeros.  Where no sequence has cached tokens, page_table_dev may be NULL (an empty table).
+ * Flags, plan and workspace as for specroll_tree_attn_paged.
  * With up to 16 query rows (N Hq / Hkv) per KV head the lengths on the device may be below the host's, so that a call captured for the
  * longest that the sequences get can be replayed as they grow.  Lengths above the host's are followed as long as the sequences need no more
  * chunks of pages than were planned for those (or none was cut); else O and lse stay as they were and the workspace's status word becomes

@@ -983,10 +983,14 @@ extern "C" int specroll_tree_attn_kv4(const specroll_attn_desc *d, const void *Q
                                       const int32_t *page_table_dev, const int32_t *page_indptr_dev, const int32_t *kv_len_dev,
                                       const int32_t *kv_len_host, const void *Kt, const void *Vt, const int32_t *parent_host, void *O,
                                       float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream) {
-    if (!d || !kv_len_host || d->B < 0 || d->B > (1 << 24) || n_pages < 0 || n_pages > (1LL << 24) || !page_table_dev)
-        return SPECROLL_EINVAL;
+    if (!d || !kv_len_host || d->B < 0 || d->B > (1 << 24) || n_pages < 0 || n_pages > (1LL << 24)) return SPECROLL_EINVAL;
     std::vector<int32_t> ip;
     if (!lengths_to_indptr(kv_len_host, d->B, &ip)) return SPECROLL_EINVAL;
+    if (!page_table_dev) {  // (no cached tokens have an empty table, whose pointer may be NULL: no word of its stand-in is read)
+        if (ip.back() > 0) return SPECROLL_EINVAL;
+        page_table_dev = page_indptr_dev;
+        if (!page_table_dev && d->B > 0) return SPECROLL_EINVAL;
+    }
     return run_tree_attn(d, Q, nullptr, nullptr, n_pages * SPECROLL_PAGE_TOKENS, nullptr, kv_len_dev, page_indptr_dev, page_table_dev, ip.data(),
                          Kt, Vt, parent_host, O, lse, workspace, workspace_bytes, cuda_stream, true, pool);
 }

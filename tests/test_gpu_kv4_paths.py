@@ -292,3 +292,12 @@ def test_few_rows_of_many_sequences_of_which_some_are_cut(N, Hq):
     assert _cut(x)
     O = _check(x)
     assert all(torch.equal(O, _run(x)) for _ in range(10))
+
+
+@pytest.mark.parametrize("N,Hq", [(1, 4), (8, 4), (30, 12)])
+def test_attention_with_nothing_cached(N, Hq):
+    """No sequence has tokens yet: an empty page table, and a pool of no pages."""
+    x = _case(3, N, Hq, 2, 64, [0, 0, 0], seed=70)
+    assert len(x["table"]) == 0
+    O = _check(x)
+    assert torch.equal(O, _run({**x, "pool": x["pool"][:0]})) and torch.equal(O, _run({**x, "table": np.array([2], np.int32)}))

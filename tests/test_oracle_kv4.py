@@ -150,6 +150,18 @@ def test_lengths_that_round_up_past_31_bits_are_refused(N, Hq, Hkv):
                                     parent.ctypes.data_as(C.c_void_p), ok, C.c_void_p(0), C.c_void_p(0), C.c_size_t(0), C.c_void_p(0)) == 1
 
 
+def test_an_empty_page_table_is_taken_where_no_tokens_are_cached():
+    L, null, _ = _null_calls()
+    ok = C.c_void_p(np.zeros(64, np.int64).ctypes.data // 16 * 16 + 16)
+
+    def call(lens, B=2, indptr=ok):
+        lens, d = np.array(lens, np.int32), S.AttnDesc(B, 1, 4, 2, 64, 0.125, 0)
+        return L.specroll_tree_attn_kv4(C.byref(d), ok, null, C.c_int64(0), null, indptr, ok, lens.ctypes.data_as(C.c_void_p), ok, ok,
+                                        np.array([-1], np.int32).ctypes.data_as(C.c_void_p), ok, null, null, C.c_size_t(0), null)
+    assert call([0, 0]) == 3                                                   # as far as the workspace, which is missing here
+    assert call([0, 1]) == 1 and call([0, 0], indptr=null) == 1 and call([], B=0, indptr=null) == 0
+
+
 def test_loading_k_and_v_to_one_place_is_refused():
     L, null, _ = _null_calls()
     base, i32, i64 = np.zeros(64, np.int64).ctypes.data // 16 * 16 + 16, C.c_int32, C.c_int64
